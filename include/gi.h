@@ -64,6 +64,7 @@ enum {
 };
 
 enum { GI_F16 = 1, GI_F32 = 2 };   /* storage type of activations (and of NHWC inputs/outputs) */
+enum { GI_BF16 = 3 };              /* operators on rows (gi_linear_q4_run, gi_log_probs) only */
 enum { GI_NHWC = 0, GI_PHWC4 = 1 }; /* layout of a caller-visible tensor */
 
 enum {
@@ -371,6 +372,41 @@ GI_API gi_status gi_slice8_pointwise_pack(const float* w, const float* bias, int
                                           uint64_t blob_bytes);
 GI_API gi_status gi_slice8_pointwise_run(const void* dev_in, void* dev_out, const void* dev_blob, int32_t batch, int32_t H,
                                          int32_t W, int32_t cin, int32_t cout, int32_t act, void* stream);
+
+/* ---- the answer's end of a network ----
+ *
+ * Operators on rows: device tensors [rows][channels] whose channels are contiguous and whose rows are `ld` elements apart.  They
+ * need no graph; a graph reaches the first one by GI_Q4 weights.  Like gi_run they enqueue on `stream` and return; they allocate
+ * nothing, keep nothing between calls and give bit-identical outputs for the same inputs.  Any number of calls may run at once on
+ * any streams.  Pointers belong to the current device and need the alignment of their elements only (blobs: 256 bytes).  Nothing
+ * is launched if an argument check fails. */
+
+/* Fully connected layer with 4-bit weights:
+ *   y[r,o] = act(bias[o] + sum_k w[o,k] x[r,k]),   w[o,k] = scale[o, k / group] * (q[o,k] - zero[o, k / group])
+ * with q and zero whole numbers of 0 .. 15.  For dtype GI_F16 and GI_BF16 products are exact and sums fp32, for each group before its
+ * scale is applied; y is rounded once.  For GI_F32 x counts with all its digits.
+ * (Section 3.2 treats the 1x1 convolution as an operator of its own; the paper has no counterpart of the weights' type.) */
+typedef struct gi_linear_q4 {
+  int32_t cin, cout;      /* up to 2^20 each */
+  int32_t group;          /* input channels that share a scale: a multiple of 32; the last group may be shorter */
+  int32_t scale_dtype;    /* GI_F16, GI_BF16 or GI_F32 */
+  int32_t has_zeros;      /* 0: every zero point is 8 */
+  int32_t dtype;          /* of x and y: GI_F16, GI_BF16 or GI_F32 */
+  int32_t act;            /* GI_ACT_* */
+} gi_linear_q4;
+
+/* Bytes of a layer's packed blob. */
+GI_API gi_status gi_linear_q4_blob_bytes(const gi_linear_q4* layer, uint64_t* bytes);
+
+/* Pack a layer (host memory) into `host_blob`, which the caller copies to the device: q [cout][(cin + 1) / 2], two values a byte, the
+ * even channel in the low half; scales and zeros (one byte each; NULL without has_zeros) [cout][ceil(cin / group)]; bias cout floats
+ * or NULL.  GI_E_INVALID for a zero point above 15. */
+GI_API gi_status gi_linear_q4_pack(const gi_linear_q4* layer, const uint8_t* q, const void* scales, const uint8_t* zeros, const float* bias,
+                                   void* host_blob, uint64_t blob_bytes);
+
+/* Enqueue the product of `rows` >= 0 rows; ldx >= cin, ldy >= cout (not looked at for rows <= 1).  x and y must not overlap. */
+GI_API gi_status gi_linear_q4_run(const gi_linear_q4* layer, const void* dev_blob, const void* dev_x, int64_t ldx, void* dev_y, int64_t ldy,
+                                  int32_t rows, void* stream);
 
 GI_API void gi_exec_destroy(gi_exec* e);
 

@@ -19,7 +19,7 @@ LIB_PATH = os.path.join(_HERE, "libgi.so")
 
 GI_OK = 0
 GI_E_INVALID, GI_E_UNSUPPORTED, GI_E_NOMEM, GI_E_CUDA, GI_E_STATE, GI_E_ARENA = -1, -2, -3, -4, -5, -6
-GI_F16, GI_F32 = 1, 2
+GI_F16, GI_F32, GI_BF16 = 1, 2, 3  # GI_BF16: operators on rows only
 GI_NHWC, GI_PHWC4 = 0, 1
 GI_OP_CONV2D, GI_OP_DEPTHWISE_CONV2D, GI_OP_ADD, GI_OP_ACTIVATION, GI_OP_GLOBAL_AVG_POOL, GI_OP_RESIZE_BILINEAR = 1, 2, 3, 4, 5, 6
 GI_OP_CONCAT = 7
@@ -73,9 +73,15 @@ class gi_launch_info(C.Structure):
     _fields_ = [("kernel", C.c_int32), ("n_ops", C.c_int32), ("bytes", C.c_uint64), ("flops", C.c_uint64)]
 
 
+class gi_linear_q4(C.Structure):
+    _fields_ = [("cin", C.c_int32), ("cout", C.c_int32), ("group", C.c_int32), ("scale_dtype", C.c_int32), ("has_zeros", C.c_int32),
+                ("dtype", C.c_int32), ("act", C.c_int32)]
+
+
 EXPORTS = ["gi_graph_create", "gi_graph_input", "gi_add_op", "gi_graph_output", "gi_graph_destroy", "gi_compile",
            "gi_exec_query", "gi_exec_tensor", "gi_exec_op", "gi_exec_launch", "gi_exec_bind", "gi_run", "gi_run_static", "gi_run_timed", "gi_device_status", "gi_selftest_bounded_wait", "gi_exec_destroy",
            "gi_slice8_tensor_bytes", "gi_slice8_pointwise_blob_bytes", "gi_slice8_pointwise_pack", "gi_slice8_pointwise_run",
+           "gi_linear_q4_blob_bytes", "gi_linear_q4_pack", "gi_linear_q4_run",
            "gi_status_str", "gi_last_error", "gi_tensor_bytes", "gi_f32_to_f16"]
 
 _lib = None
@@ -128,6 +134,12 @@ def lib() -> C.CDLL:
     L.gi_slice8_pointwise_pack.restype = C.c_int32
     L.gi_slice8_pointwise_run.argtypes = [vp, vp, vp] + [C.c_int32] * 6 + [vp]
     L.gi_slice8_pointwise_run.restype = C.c_int32
+    L.gi_linear_q4_blob_bytes.argtypes = [C.POINTER(gi_linear_q4), C.POINTER(C.c_uint64)]
+    L.gi_linear_q4_blob_bytes.restype = C.c_int32
+    L.gi_linear_q4_pack.argtypes = [C.POINTER(gi_linear_q4), vp, vp, vp, vp, vp, C.c_uint64]
+    L.gi_linear_q4_pack.restype = C.c_int32
+    L.gi_linear_q4_run.argtypes = [C.POINTER(gi_linear_q4), vp, vp, C.c_int64, vp, C.c_int64, C.c_int32, vp]
+    L.gi_linear_q4_run.restype = C.c_int32
     L.gi_status_str.argtypes = [C.c_int32]
     L.gi_status_str.restype = C.c_char_p
     L.gi_last_error.argtypes = []
@@ -192,6 +204,91 @@ def gi_slice8_pointwise_pack(w: np.ndarray, bias: np.ndarray) -> np.ndarray:
 def gi_slice8_pointwise_run(dev_in: int, dev_out: int, dev_blob: int, batch, H, W, cin, cout, act, stream=None) -> None:
     """Argument marshalling only: the three pointers are device addresses (torch tensors' data_ptr())."""
     _check(lib().gi_slice8_pointwise_run(dev_in, dev_out, dev_blob, batch, H, W, cin, cout, act, _stream_ptr(stream)), "gi_slice8_pointwise_run")
+
+
+def _torch_dtype(dtype: int):
+    import torch
+    return {GI_F16: torch.float16, GI_BF16: torch.bfloat16, GI_F32: torch.float32}[dtype]
+
+
+def _gi_dtype(t) -> int:
+    """GI_* of a torch tensor's element type (0 where the library has none)."""
+    import torch
+    return {torch.float16: GI_F16, torch.bfloat16: GI_BF16, torch.float32: GI_F32}.get(t.dtype, 0)
+
+
+def _host(t, what: str, dtypes, shape):
+    """`t` (torch tensor on any device, or numpy array) as a contiguous host tensor of one of `dtypes` and of `shape`."""
+    import torch
+    t = torch.from_numpy(np.ascontiguousarray(t)) if isinstance(t, np.ndarray) else t
+    if t.dtype not in dtypes or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: need {' or '.join(str(d) for d in dtypes)} of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    return t.detach().cpu().contiguous()
+
+
+def _rows(t, what: str, dtype, channels: int, device):
+    """(pointer, elements between rows, rows) of a device tensor [..., channels] whose leading axes form rows at one pitch."""
+    if t.dtype != dtype or t.device != device or t.dim() < 1 or t.shape[-1] != channels:
+        raise ValueError(f"{what}: need {dtype} of shape [..., {channels}] on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if t.dim() == 2:
+        if t.stride(1) == 1 or channels == 1:
+            return t.data_ptr(), t.stride(0), t.shape[0]
+    elif t.is_contiguous():
+        return t.data_ptr(), channels, t.numel() // channels
+    raise ValueError(f"{what}: channels must be contiguous, and all of a tensor of other than two axes (strides {t.stride()})")
+
+
+def _on(device, stream, call):
+    """call(stream handle) with `device` current: the library launches on the current device."""
+    import torch
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+    if torch.cuda.current_device() == device.index:
+        return call(handle)
+    with torch.cuda.device(device):
+        return call(handle)
+
+
+class LinearQ4:
+    """gi_linear_q4_*: a fully connected layer with 4-bit weights, kept on a device.
+
+    q [cout, (cin + 1) / 2] uint8, two values a byte, the even input channel in the low half; scales [cout, ceil(cin / group)] float16,
+    bfloat16 or float32; zeros (optional, else 8 everywhere) uint8 of the scales' shape, 0 .. 15; bias (optional) [cout] float32.
+    Tensors on any device, or numpy arrays; they are copied.  `dtype` is the type of the rows that run() takes and returns.
+    """
+
+    def __init__(self, q, scales, zeros=None, bias=None, *, cin: int, group: int, dtype: int = GI_F16, act: int = GI_ACT_NONE,
+                 device="cuda:0"):
+        import torch
+        cout, groups = int(q.shape[0]), -(-cin // group) if group > 0 else 0
+        q = _host(q, "q", (torch.uint8,), (cout, (cin + 1) // 2))
+        scales = _host(scales, "scales", (torch.float16, torch.bfloat16, torch.float32), (cout, groups))
+        zeros = None if zeros is None else _host(zeros, "zeros", (torch.uint8,), (cout, groups))
+        bias = None if bias is None else _host(bias, "bias", (torch.float32,), (cout,))
+        self.desc = gi_linear_q4(cin, cout, group, _gi_dtype(scales), 0 if zeros is None else 1, dtype, act)
+        self._ref = C.byref(self.desc)
+        n = C.c_uint64(0)
+        _check(lib().gi_linear_q4_blob_bytes(self._ref, C.byref(n)), "gi_linear_q4_blob_bytes")
+        blob = torch.empty(int(n.value), dtype=torch.uint8)
+        _check(lib().gi_linear_q4_pack(self._ref, q.data_ptr(), scales.data_ptr(), None if zeros is None else zeros.data_ptr(),
+                                       None if bias is None else bias.data_ptr(), blob.data_ptr(), blob.numel()), "gi_linear_q4_pack")
+        self.cin, self.cout, self.dtype = cin, cout, _torch_dtype(dtype)
+        self.blob = blob.to(device)
+        self.device = self.blob.device
+
+    def run(self, x, y=None, stream=None):
+        """y[..., cout] = act(x[..., cin] w^T + bias) on `stream` (default: the current one of the layer's device); y is made where none is given.
+        Two axes may have any distance between rows; other tensors are contiguous."""
+        import torch
+        if y is None:
+            y = torch.empty(tuple(x.shape[:-1]) + (self.cout,), dtype=self.dtype, device=self.device)
+        xp, ldx, rows = _rows(x, "x", self.dtype, self.cin, self.device)
+        yp, ldy, yrows = _rows(y, "y", self.dtype, self.cout, self.device)
+        if rows != yrows:
+            raise ValueError(f"x has {rows} rows, y {yrows}")
+        _check(_on(self.device, stream, lambda s: lib().gi_linear_q4_run(self._ref, self.blob.data_ptr(), xp, ldx, yp, ldy, rows, s)), "gi_linear_q4_run")
+        return y
 
 
 class Graph:

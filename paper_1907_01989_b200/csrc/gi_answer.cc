@@ -1,0 +1,108 @@
+// C ABI of the operators on rows: 4-bit linear layers and log probabilities of classes.  Argument checks only; the kernels are in
+// linear_q4.cu and log_probs.cu.
+#include <cuda_runtime.h>
+
+#include <string>
+
+#include "gi_internal.h"
+#include "kernels.h"
+
+using namespace gi;
+
+namespace {
+
+int elem_of(int dtype) { return dtype == GI_F32 ? 4 : 2; }
+bool known_dtype(int dtype) { return dtype == GI_F16 || dtype == GI_BF16 || dtype == GI_F32; }
+bool aligned_to(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % static_cast<unsigned>(bytes) == 0; }
+
+gi_status check_layer(const char* who, const gi_linear_q4* l) {
+  const std::string w(who);
+  if (!l) return fail(GI_E_INVALID, w + ": null layer");
+  if (l->cin <= 0 || l->cout <= 0) return fail(GI_E_INVALID, w + ": cin and cout must be positive");
+  if (l->cin > (1 << 20) || l->cout > (1 << 20)) return fail(GI_E_UNSUPPORTED, w + ": cin or cout above 2^20");
+  if (l->group <= 0) return fail(GI_E_INVALID, w + ": group must be positive");
+  if (l->group % 32 != 0) return fail(GI_E_UNSUPPORTED, w + ": group must be a multiple of 32");
+  if (!known_dtype(l->scale_dtype)) return fail(GI_E_INVALID, w + ": scale_dtype must be GI_F16, GI_BF16 or GI_F32");
+  if (!known_dtype(l->dtype)) return fail(GI_E_INVALID, w + ": dtype must be GI_F16, GI_BF16 or GI_F32");
+  if (l->has_zeros != 0 && l->has_zeros != 1) return fail(GI_E_INVALID, w + ": has_zeros must be 0 or 1");
+  if (l->act != GI_ACT_NONE && l->act != GI_ACT_RELU && l->act != GI_ACT_RELU6) return fail(GI_E_INVALID, w + ": unknown activation");
+  return GI_OK;
+}
+
+// bytes from the first to behind the last element of a tensor of rows
+uint64_t extent(int64_t rows, int64_t ld, int64_t n, int elem) { return (static_cast<uint64_t>(rows - 1) * ld + n) * elem; }
+
+bool overlap(const void* a, uint64_t na, const void* b, uint64_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + nb && y < x + na;
+}
+
+constexpr int64_t kMaxPitch = int64_t{1} << 30;  // elements between rows: with 2^31 rows and 4 bytes, below 2^63 bytes
+
+}  // namespace
+
+extern "C" {
+
+gi_status gi_linear_q4_blob_bytes(const gi_linear_q4* layer, uint64_t* bytes) {
+  const gi_status st = check_layer("gi_linear_q4_blob_bytes", layer);
+  if (st != GI_OK) return st;
+  if (!bytes) return fail(GI_E_INVALID, "gi_linear_q4_blob_bytes: null argument");
+  *bytes = linear_q4_layout(layer->cin, layer->cout, layer->group, layer->scale_dtype, layer->has_zeros != 0).bytes;
+  return GI_OK;
+}
+
+gi_status gi_linear_q4_pack(const gi_linear_q4* layer, const uint8_t* q, const void* scales, const uint8_t* zeros, const float* bias,
+                            void* host_blob, uint64_t blob_bytes) {
+  const gi_status st = check_layer("gi_linear_q4_pack", layer);
+  if (st != GI_OK) return st;
+  if (!q || !scales || !host_blob) return fail(GI_E_INVALID, "gi_linear_q4_pack: null argument");
+  if ((zeros != nullptr) != (layer->has_zeros != 0)) return fail(GI_E_INVALID, "gi_linear_q4_pack: zeros must be given exactly where has_zeros is 1");
+  const LinearQ4Layout l = linear_q4_layout(layer->cin, layer->cout, layer->group, layer->scale_dtype, zeros != nullptr);
+  if (blob_bytes < l.bytes) return fail(GI_E_INVALID, "gi_linear_q4_pack: host_blob too small");
+  if (zeros) {
+    const size_t n = static_cast<size_t>(layer->cout) * l.n_groups;
+    for (size_t i = 0; i < n; ++i)
+      if (zeros[i] > 15) return fail(GI_E_INVALID, "gi_linear_q4_pack: zero point above 15");
+  }
+  linear_q4_pack(LinearQ4Weights{q, scales, zeros, layer->cin, layer->cout, layer->group, layer->scale_dtype}, bias, static_cast<uint8_t*>(host_blob));
+  return GI_OK;
+}
+
+gi_status gi_linear_q4_run(const gi_linear_q4* layer, const void* dev_blob, const void* dev_x, int64_t ldx, void* dev_y, int64_t ldy,
+                           int32_t rows, void* stream) {
+  const gi_status st = check_layer("gi_linear_q4_run", layer);
+  if (st != GI_OK) return st;
+  if (rows < 0) return fail(GI_E_INVALID, "gi_linear_q4_run: negative number of rows");
+  if (rows == 0) return GI_OK;
+  if (!dev_blob || !dev_x || !dev_y) return fail(GI_E_INVALID, "gi_linear_q4_run: null argument");
+  const int elem = elem_of(layer->dtype);
+  if (!aligned_to(dev_blob, 256)) return fail(GI_E_INVALID, "gi_linear_q4_run: the blob must be 256-byte aligned");
+  if (!aligned_to(dev_x, elem) || !aligned_to(dev_y, elem)) return fail(GI_E_INVALID, "gi_linear_q4_run: x or y not aligned to its elements");
+  if (rows == 1) {
+    ldx = layer->cin;
+    ldy = layer->cout;
+  }
+  if (ldx < layer->cin || ldy < layer->cout) return fail(GI_E_INVALID, "gi_linear_q4_run: rows overlap (ldx < cin or ldy < cout)");
+  if (ldx > kMaxPitch || ldy > kMaxPitch) return fail(GI_E_INVALID, "gi_linear_q4_run: ldx or ldy too large");
+  if (overlap(dev_x, extent(rows, ldx, layer->cin, elem), dev_y, extent(rows, ldy, layer->cout, elem)))
+    return fail(GI_E_INVALID, "gi_linear_q4_run: x and y overlap");
+  LinearQ4Call c;
+  c.blob = dev_blob;
+  c.x = dev_x;
+  c.y = dev_y;
+  c.x_row = ldx;
+  c.y_row = ldy;
+  c.rows = rows;
+  c.cin = layer->cin;
+  c.cout = layer->cout;
+  c.group = layer->group;
+  c.scale_dtype = layer->scale_dtype;
+  c.dtype = layer->dtype;
+  c.zeros = layer->has_zeros != 0;
+  c.ep.act_pre = layer->act;
+  const int err = launch_linear_q4(c, stream);
+  if (err != 0) return fail(GI_E_CUDA, std::string("gi_linear_q4_run: ") + cudaGetErrorString(static_cast<cudaError_t>(err)));
+  return GI_OK;
+}
+
+}  // extern "C"

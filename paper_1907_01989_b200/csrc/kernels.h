@@ -130,4 +130,32 @@ void pointwise_mma_pack(const float* w, const float* bias, int cin, int cout, st
 int launch_pointwise_mma(const LaunchRec& r, const Ptrs& p, void** state, int launch_index, void* stream);
 unsigned int pointwise_mma_error_word(int* cuda_err);
 
+// Fully connected layer with 4-bit weights (linear_q4.cu).  The caller's weights: q two values a byte, [cout][(cin + 1) / 2];
+// scales (and zeros or null: 8 everywhere) [cout][ceil(cin / group)]; `group` a multiple of 32.
+struct LinearQ4Weights {
+  const uint8_t* q = nullptr;
+  const void* scales = nullptr;
+  const uint8_t* zeros = nullptr;
+  int cin = 0, cout = 0, group = 0, scale_dtype = GI_F16;
+};
+// byte offsets inside the packed blob (weights at 0), its size, and how many units it holds
+struct LinearQ4Layout {
+  int n_blocks = 0, n_units = 0, n_groups = 0;
+  uint64_t scales = 0, zeros = 0, bias = 0, bytes = 0;
+};
+// One product.  Rows of x and y are `x_row` / `y_row` elements apart, channels contiguous; or, with x_slice / y_slice > 0, both lie in
+// slices of 4 channels (rows are stored pixels).  plane > 0: y is the caller's NHWC tensor, its pixels `real` of `plane` stored ones.
+struct LinearQ4Call {
+  const void *blob = nullptr, *x = nullptr, *res = nullptr;
+  void* y = nullptr;
+  long long x_row = 0, x_slice = 0, y_row = 0, y_slice = 0;
+  int rows = 0, cin = 0, cout = 0, group = 0, scale_dtype = GI_F16, dtype = GI_F16;
+  bool zeros = false;
+  int plane = 0, real = 0;
+  Epilogue ep;
+};
+LinearQ4Layout linear_q4_layout(int cin, int cout, int group, int scale_dtype, bool zeros);
+void linear_q4_pack(const LinearQ4Weights& w, const float* bias, uint8_t* blob);  // blob: layout.bytes bytes
+int launch_linear_q4(const LinearQ4Call& c, void* stream);
+
 }  // namespace gi

@@ -1,0 +1,284 @@
+"""Fully connected layers with 4-bit weights: gi_linear_q4_* against a plain form in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import answer_ref as ref
+from paper_1907_01989_b200 import api
+
+GI = {torch.float16: api.GI_F16, torch.bfloat16: api.GI_BF16, torch.float32: api.GI_F32}
+ACT = {"none": api.GI_ACT_NONE, "relu": api.GI_ACT_RELU, "relu6": api.GI_ACT_RELU6}
+
+
+def rows_of(seed, rows, cin, dtype):
+    return torch.randn((rows, cin), generator=torch.Generator().manual_seed(seed)).to(dtype)
+
+
+def check(x, layer, weights, group, act="none", y=None):
+    got = layer.run(x.cuda(), y)
+    torch.cuda.synchronize()
+    want, bound = ref.linear_q4(x, *weights, group, act)
+    err = (got.double().cpu() - want).abs()
+    assert got.dtype == x.dtype and torch.isfinite(got).all()
+    assert (err <= bound).all(), f"worst {(err / bound).max().item():.3f} of the bound"
+    return got
+
+
+def make(seed, cin, cout, group, dtype, scale=torch.float16, zeros=False, bias=True, act="none", device="cuda:0"):
+    weights = ref.q4_layer(seed, cin, cout, group, scale, zeros, bias)
+    q, s, z, b = weights
+    return api.LinearQ4(q, s, z, b, cin=cin, group=group, dtype=GI[dtype], act=ACT[act], device=device), weights
+
+
+# ---------------------------------------------------------------- host
+def unpack_blob(blob, cin, cout, group, scale_bytes, zeros):
+    """q, scale bytes and zero points out of a packed blob: the layout that the kernel's comment states, restated."""
+    nb, nu, ng = -(-cout // 16), -(-cin // 64), -(-cin // group)
+    up = lambda v: -(-v // 256) * 256  # noqa: E731
+    words = blob[:nb * nu * 512].view(np.uint32).reshape(nb, nu, 8, 4, 4)  # block, unit, g, t, word
+    q = np.zeros((nb * 16, nu * 64), dtype=np.uint8)
+    for s in range(4):
+        for nib in range(8):
+            row, off = nib % 2, 2 * (nib % 4 // 2) + nib // 4  # row g or g + 8; channel within four
+            v = (words[..., s] >> (4 * nib)) & 15
+            for t in range(4):
+                k = 32 * (s // 2) + 8 * t + 4 * (s % 2) + off
+                q.reshape(nb, 2, 8, nu, 64)[:, row, :, :, k] = v[..., t].transpose(0, 2, 1)
+    at = up(nb * nu * 512)
+    pairs = lambda a, n: a.reshape(nb, ng, 8, 2, n).transpose(0, 3, 2, 1, 4).reshape(nb * 16, ng, n)[:cout]  # noqa: E731
+    sc = pairs(blob[at:at + nb * ng * 16 * scale_bytes], scale_bytes)
+    at = up(at + nb * ng * 16 * scale_bytes)
+    z = pairs(blob[at:at + nb * ng * 16], 1)[..., 0] if zeros else None
+    at = up(at + (nb * ng * 16 if zeros else 0))
+    bias = blob[at:at + nb * 64].view(np.float32)[:cout]
+    return q[:cout, :cin], sc, z, bias
+
+
+@pytest.mark.parametrize("cin,cout,group,scale,zeros", [(64, 16, 32, torch.float16, False), (1, 1, 32, torch.float32, True), (97, 33, 32, torch.float16, True),
+                                                        (1280, 41, 96, torch.bfloat16, True), (200, 17, 256, torch.float32, False)])
+def test_pack_keeps_every_value_in_its_place(cin, cout, group, scale, zeros):
+    layer, (q, s, z, b) = make(3, cin, cout, group, torch.float16, scale, zeros, device="cpu")
+    sb = s.element_size()
+    got_q, got_s, got_z, got_b = unpack_blob(layer.blob.numpy(), cin, cout, group, sb, zeros)
+    assert np.array_equal(got_q, torch.stack([q & 15, q >> 4], -1).flatten(1)[:, :cin].numpy())
+    assert np.array_equal(got_s, s.view(torch.uint8).reshape(cout, -1, sb).numpy())
+    assert not zeros or np.array_equal(got_z, z.numpy())
+    assert np.array_equal(got_b, b.numpy())
+
+
+def test_refusals_of_a_layer():
+    import ctypes as C
+    L, n = api.lib(), C.c_uint64(0)
+
+    def status(**kw):
+        d = dict(cin=64, cout=32, group=32, scale_dtype=api.GI_F16, has_zeros=0, dtype=api.GI_F16, act=0)
+        d.update(kw)
+        return L.gi_linear_q4_blob_bytes(C.byref(api.gi_linear_q4(**d)), C.byref(n))
+
+    assert status() == api.GI_OK and n.value > 0
+    for bad in (dict(cin=0), dict(cout=-1), dict(group=0), dict(scale_dtype=4), dict(dtype=0), dict(act=7), dict(has_zeros=2)):
+        assert status(**bad) == api.GI_E_INVALID, bad
+    for bad in (dict(group=16), dict(group=48), dict(cin=(1 << 20) + 1), dict(cout=(1 << 20) + 1)):
+        assert status(**bad) == api.GI_E_UNSUPPORTED, bad
+    assert L.gi_linear_q4_blob_bytes(None, C.byref(n)) == api.GI_E_INVALID
+    assert L.gi_linear_q4_blob_bytes(C.byref(api.gi_linear_q4(64, 32, 32, 1, 0, 1, 0)), None) == api.GI_E_INVALID
+
+
+def test_refusals_of_pack():
+    q, s, z, b = ref.q4_layer(1, 64, 16, 32, zeros=True)
+    z[3, 1] = 16
+    with pytest.raises(api.GiError) as e:
+        api.LinearQ4(q, s, z, b, cin=64, group=32, device="cpu")
+    assert e.value.status == api.GI_E_INVALID and "above 15" in str(e.value)
+    for kw in (dict(cin=66), dict(group=64)):
+        with pytest.raises(ValueError):
+            api.LinearQ4(q, s, None, b, **{"cin": 64, "group": 32, "device": "cpu", **kw})
+    with pytest.raises(ValueError):
+        api.LinearQ4(q, s.double(), None, b, cin=64, group=32, device="cpu")
+    import ctypes as C
+    d = api.gi_linear_q4(64, 16, 32, api.GI_F16, 1, api.GI_F16, 0)
+    buf = torch.empty(1 << 14, dtype=torch.uint8)
+    L = api.lib()
+    assert L.gi_linear_q4_pack(C.byref(d), q.data_ptr(), s.data_ptr(), None, None, buf.data_ptr(), buf.numel()) == api.GI_E_INVALID  # zeros missing
+    d.has_zeros = 0
+    assert L.gi_linear_q4_pack(C.byref(d), q.data_ptr(), s.data_ptr(), None, None, buf.data_ptr(), 100) == api.GI_E_INVALID  # too small
+    assert L.gi_linear_q4_pack(C.byref(d), None, s.data_ptr(), None, None, buf.data_ptr(), buf.numel()) == api.GI_E_INVALID
+
+
+def test_refusals_of_run_before_any_launch():
+    """Checked on the host: nothing here reaches a device."""
+    import ctypes as C
+    L = api.lib()
+    d = api.gi_linear_q4(64, 32, 32, api.GI_F16, 0, api.GI_F16, 0)
+    blob, x, y = 0x100000, 0x200000, 0x300000
+
+    def run(blob=blob, x=x, ldx=64, y=y, ldy=32, rows=4):
+        return L.gi_linear_q4_run(C.byref(d), blob, x, ldx, y, ldy, rows, None)
+
+    assert run(rows=0) == api.GI_OK  # no rows: nothing to do
+    for bad in (dict(rows=-1), dict(blob=None), dict(x=None), dict(y=None), dict(blob=blob + 128), dict(x=x + 1), dict(y=y + 1), dict(ldx=63),
+                dict(ldy=31), dict(ldx=(1 << 30) + 1), dict(y=x), dict(y=x + 64 * 2 * 3), dict(x=y + 32 * 2 * 3)):
+        assert run(**bad) == api.GI_E_INVALID, bad
+
+
+# ---------------------------------------------------------------- GPU
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows", [1, 2, 3, 5, 8, 9, 16, 17, 31, 40, 130])
+def test_rows(rows, dtype):
+    layer, w = make(rows, 320, 200, 64, dtype)
+    check(rows_of(rows, rows, 320, dtype), layer, w, 64)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cin,cout", [(1, 1), (2, 3), (31, 16), (33, 17), (63, 15), (64, 128), (65, 129), (1000, 1001), (1280, 1001), (4099, 70), (9000, 40), (130, 5000)])
+@pytest.mark.parametrize("dtype,rows", [(torch.float16, 1), (torch.bfloat16, 7), (torch.float32, 4), (torch.float16, 33)])
+def test_sizes(cin, cout, dtype, rows):
+    layer, w = make(cin + cout, cin, cout, 32, dtype, zeros=True)
+    check(rows_of(7, rows, cin, dtype), layer, w, 32)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("group", [32, 64, 96, 128, 160, 1024, 1 << 30])
+@pytest.mark.parametrize("scale", [torch.float16, torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("zeros", [False, True])
+def test_groups_scales_and_zero_points(group, scale, zeros):
+    for dtype, rows in ((torch.float16, 2), (torch.bfloat16, 12), (torch.float32, 1), (torch.bfloat16, 70)):
+        layer, w = make(group % 1000, 710, 50, group, dtype, scale, zeros)
+        check(rows_of(1, rows, 710, dtype), layer, w, group)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act", ["none", "relu", "relu6"])
+@pytest.mark.parametrize("bias", [False, True])
+def test_epilogue(act, bias):
+    layer, w = make(5, 256, 96, 128, torch.float16, bias=bias, act=act)
+    x = rows_of(2, 6, 256, torch.float16) * 20
+    got = check(x, layer, w, 128, act)
+    assert act == "none" or (got == 0).any()
+    assert act != "relu6" or got.max() <= 6
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("off", [0, 1, 3])
+@pytest.mark.parametrize("rows", [3, 40])
+def test_rows_inside_wider_tensors(dtype, off, rows):
+    """Any pitch and any alignment of the elements; what lies beside the rows is neither used nor written."""
+    cin, cout = 200, 77
+    layer, w = make(9, cin, cout, 64, dtype)
+    x = rows_of(3, rows, cin, dtype)
+    wide = torch.full((rows, cin + 13), float("nan"), dtype=dtype, device="cuda")
+    wide[:, off:off + cin] = x.cuda()
+    out = torch.full((rows + 1, cout + 9), 123.0, dtype=dtype, device="cuda")
+    y = out[:rows, off:off + cout]
+    got = layer.run(wide[:, off:off + cin], y)
+    assert got.data_ptr() == y.data_ptr()
+    want, bound = ref.linear_q4(x, *w, 64)
+    assert ((y.double().cpu() - want).abs() <= bound).all()
+    out[:rows, off:off + cout] = 123.0
+    assert (out == 123.0).all()
+
+
+@pytest.mark.gpu
+def test_32_bit_rows_count_with_all_their_digits():
+    """x = 1 + 2^-23 against x = 1: the difference of the results is that of the inputs, times the weights."""
+    cin, cout = 64, 16
+    q = torch.full((cout, cin // 2), 0x99, dtype=torch.uint8)  # q = 9: weights of one scale
+    layer = api.LinearQ4(q, torch.ones((cout, 1)), cin=cin, group=64, dtype=api.GI_F32)
+    x = torch.zeros((3, cin), device="cuda")
+    x[0, 5], x[1, 5], x[2, 5] = 1.0, 1.0 + 2.0 ** -23, 2.0 ** -100 * (1 + 2.0 ** -23)
+    y = layer.run(x).double().cpu()
+    assert (y[0] == 1.0).all() and (y[1] == 1.0 + 2.0 ** -23).all()
+    assert (y[2] == 2.0 ** -100 * (1 + 2.0 ** -23)).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows", [4, 40])
+def test_infinity_and_nan_stay_in_their_row(dtype, rows):
+    layer, w = make(4, 128, 48, 32, dtype)
+    x = rows_of(4, rows, 128, dtype)
+    clean = layer.run(x.cuda())
+    x[1, 17], x[2, 99] = float("inf"), float("nan")
+    got = layer.run(x.cuda())
+    keep = [r for r in range(rows) if r not in (1, 2)]
+    assert torch.equal(got[keep], clean[keep])
+    assert not torch.isfinite(got[1]).any() and torch.isnan(got[2]).all()
+
+
+@pytest.mark.gpu
+def test_no_rows_and_leading_axes():
+    layer, w = make(6, 96, 40, 32, torch.float16)
+    assert layer.run(torch.empty((0, 96), dtype=torch.float16, device="cuda")).shape == (0, 40)
+    x = rows_of(6, 12, 96, torch.float16)
+    got = layer.run(x.view(2, 2, 3, 96).cuda())
+    assert got.shape == (2, 2, 3, 40) and torch.equal(got.view(12, 40), layer.run(x.cuda()))
+    one = layer.run(x[0].cuda())
+    want, bound = ref.linear_q4(x[:1], *w, 32)
+    assert one.shape == (40,) and ((one.double().cpu() - want[0]).abs() <= bound[0]).all()
+
+
+@pytest.mark.gpu
+def test_refusals_of_the_binding():
+    layer, _ = make(6, 96, 40, 32, torch.float16)
+    x = torch.zeros((4, 96), dtype=torch.float16, device="cuda")
+    for bad in (x.float(), x[:, :95], x.cpu(), torch.zeros((96, 4), dtype=torch.float16, device="cuda").t(), x.view(2, 2, 96)[:, :, ::2]):
+        with pytest.raises(ValueError):
+            layer.run(bad)
+    with pytest.raises(ValueError):
+        layer.run(x, torch.empty((3, 40), dtype=torch.float16, device="cuda"))
+    with pytest.raises(api.GiError):
+        layer.run(x, x.view(-1)[:160].view(4, 40))  # y on x
+    with pytest.raises(api.GiError):
+        layer.run(x[:1].expand(4, 96))  # rows at distance 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [1, 20, 100])
+def test_same_bits_every_time_on_streams_and_in_graphs(rows):
+    layer, w = make(8, 1024, 500, 128, torch.float16)
+    x = rows_of(8, rows, 1024, torch.float16).cuda()
+    want = layer.run(x)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    outs = []
+    for i in range(9):
+        with torch.cuda.stream(streams[i % 3]):
+            outs.append(layer.run(x))
+    explicit = torch.empty_like(want)
+    layer.run(x, explicit, stream=streams[0])
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs + [explicit])
+    y, y2 = torch.zeros_like(want), torch.zeros_like(want)
+    graphs = []
+    for out in (y, y2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            layer.run(x, out)
+        graphs.append(g)
+    x.mul_(2)  # exact in fp16 here: a replay reads what is there now
+    with torch.cuda.stream(streams[1]):
+        graphs[1].replay()
+    graphs[0].replay()
+    torch.cuda.synchronize()
+    again = layer.run(x)
+    assert torch.equal(y, again) and torch.equal(y2, again) and not torch.equal(again, want)
+
+
+@pytest.mark.gpu
+def test_a_blob_written_just_before_the_call_is_the_one_used():
+    """The kernel may start before its predecessor has ended: it must not have read the weights by then."""
+    a, w = make(10, 2048, 512, 64, torch.float16)
+    b, _ = make(11, 2048, 512, 64, torch.float16)
+    x = rows_of(10, 1, 2048, torch.float16).cuda()
+    ya, yb = a.run(x), b.run(x)
+    torch.cuda.synchronize()
+    keep = a.blob.clone()
+    flip = keep ^ b.blob
+    for i in range(20):
+        y0 = a.run(x)
+        a.blob.bitwise_xor_(flip)  # a kernel of torch turns one layer into the other
+        y1 = a.run(x)
+        a.blob.bitwise_xor_(flip)
+        assert torch.equal(y0, ya) and torch.equal(y1, yb), i
