@@ -47,7 +47,7 @@ gi_status gi_linear_q4_blob_bytes(const gi_linear_q4* layer, uint64_t* bytes) {
   const gi_status st = check_layer("gi_linear_q4_blob_bytes", layer);
   if (st != GI_OK) return st;
   if (!bytes) return fail(GI_E_INVALID, "gi_linear_q4_blob_bytes: null argument");
-  *bytes = linear_q4_layout(layer->cin, layer->cout, layer->group, layer->scale_dtype, layer->has_zeros != 0).bytes;
+  *bytes = linear_q4_layout(layer->cin, layer->cout, layer->group, layer->scale_dtype, layer->has_zeros != 0, layer->dtype).bytes;
   return GI_OK;
 }
 
@@ -57,14 +57,14 @@ gi_status gi_linear_q4_pack(const gi_linear_q4* layer, const uint8_t* q, const v
   if (st != GI_OK) return st;
   if (!q || !scales || !host_blob) return fail(GI_E_INVALID, "gi_linear_q4_pack: null argument");
   if ((zeros != nullptr) != (layer->has_zeros != 0)) return fail(GI_E_INVALID, "gi_linear_q4_pack: zeros must be given exactly where has_zeros is 1");
-  const LinearQ4Layout l = linear_q4_layout(layer->cin, layer->cout, layer->group, layer->scale_dtype, zeros != nullptr);
+  const LinearQ4Layout l = linear_q4_layout(layer->cin, layer->cout, layer->group, layer->scale_dtype, zeros != nullptr, layer->dtype);
   if (blob_bytes < l.bytes) return fail(GI_E_INVALID, "gi_linear_q4_pack: host_blob too small");
   if (zeros) {
-    const size_t n = static_cast<size_t>(layer->cout) * l.n_groups;
+    const size_t n = static_cast<size_t>(layer->cout) * ((static_cast<int64_t>(layer->cin) + layer->group - 1) / layer->group);
     for (size_t i = 0; i < n; ++i)
       if (zeros[i] > 15) return fail(GI_E_INVALID, "gi_linear_q4_pack: zero point above 15");
   }
-  linear_q4_pack(LinearQ4Weights{q, scales, zeros, layer->cin, layer->cout, layer->group, layer->scale_dtype}, bias, static_cast<uint8_t*>(host_blob));
+  linear_q4_pack(LinearQ4Weights{q, scales, zeros, layer->cin, layer->cout, layer->group, layer->scale_dtype, layer->dtype}, bias, static_cast<uint8_t*>(host_blob));
   return GI_OK;
 }
 

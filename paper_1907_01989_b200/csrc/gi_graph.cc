@@ -44,6 +44,30 @@ uint16_t f32_to_f16_rne(float f) {
   return static_cast<uint16_t>(sign | (q + up));
 }
 
+float f16_to_f32(uint16_t h) {
+  const uint32_t s = (h & 0x8000u) << 16, e = (h >> 10) & 0x1fu, m = h & 0x3ffu;
+  uint32_t u;
+  float v;
+  if (e == 0) {
+    v = static_cast<float>(m) * (1.0f / 16777216.0f);
+    std::memcpy(&u, &v, 4);
+  } else if (e == 31) {
+    u = 0x7f800000u | (m << 13);
+  } else {
+    u = ((e + 112u) << 23) | (m << 13);
+  }
+  u |= s;
+  std::memcpy(&v, &u, 4);
+  return v;
+}
+
+float bf16_to_f32(uint16_t h) {
+  const uint32_t u = static_cast<uint32_t>(h) << 16;
+  float v;
+  std::memcpy(&v, &u, 4);
+  return v;
+}
+
 static int conv_out(int in, int k, int stride, int dil, int p0, int p1) {
   const int span = (k - 1) * dil + 1;
   const int padded = in + p0 + p1;
@@ -178,24 +202,7 @@ static gi_status add_op_checked(gi_graph* g, const gi_op_desc* desc, gi_tensor* 
         std::memcpy(node.weights.data(), desc->weights, nw * sizeof(float));
       } else {
         const uint16_t* h = static_cast<const uint16_t*>(desc->weights);
-        for (size_t i = 0; i < nw; ++i) {
-          // widen fp16 bits to fp32 exactly
-          const uint32_t s = (h[i] & 0x8000u) << 16, e = (h[i] >> 10) & 0x1fu, m = h[i] & 0x3ffu;
-          float v;
-          if (e == 0) {
-            v = static_cast<float>(m) * (1.0f / 16777216.0f);
-          } else if (e == 31) {
-            const uint32_t u = 0x7f800000u | (m << 13);
-            std::memcpy(&v, &u, 4);
-          } else {
-            const uint32_t u = ((e + 112u) << 23) | (m << 13);
-            std::memcpy(&v, &u, 4);
-          }
-          uint32_t u;
-          std::memcpy(&u, &v, 4);
-          u |= s;
-          std::memcpy(&node.weights[i], &u, 4);
-        }
+        for (size_t i = 0; i < nw; ++i) node.weights[i] = f16_to_f32(h[i]);
       }
       node.bias.assign(cout, 0.0f);
       if (desc->bias) std::memcpy(node.bias.data(), desc->bias, cout * sizeof(float));

@@ -178,6 +178,8 @@ inline int slices(int c) { return (c + 3) / 4; }
 inline int elem_bytes(int storage) { return storage == GI_F32 ? 4 : 2; }
 
 uint16_t f32_to_f16_rne(float f);
+float f16_to_f32(uint16_t h);   // exact
+float bf16_to_f32(uint16_t h);  // exact
 
 // compile-step pieces (gi_compile.cc)
 gi_status fuse_graph(const gi_graph& g, bool enable, std::vector<FusedOp>* out);

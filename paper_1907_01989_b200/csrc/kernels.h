@@ -136,12 +136,13 @@ struct LinearQ4Weights {
   const uint8_t* q = nullptr;
   const void* scales = nullptr;
   const uint8_t* zeros = nullptr;
-  int cin = 0, cout = 0, group = 0, scale_dtype = GI_F16;
+  int cin = 0, cout = 0, group = 0, scale_dtype = GI_F16, dtype = GI_F16;
 };
-// byte offsets inside the packed blob (weights at 0), its size, and how many units it holds
+// the packed blob: n_blocks x n_units records, then the bias
 struct LinearQ4Layout {
-  int n_blocks = 0, n_units = 0, n_groups = 0;
-  uint64_t scales = 0, zeros = 0, bias = 0, bytes = 0;
+  int n_blocks = 0, n_units = 0, parts = 1;  // parts of a record with a scale of their own
+  int record = 0, zeros_at = 0;              // bytes of a record, of what lies in front of its zero points
+  uint64_t bias = 0, bytes = 0;
 };
 // One product.  Rows of x and y are `x_row` / `y_row` elements apart, channels contiguous; or, with x_slice / y_slice > 0, both lie in
 // slices of 4 channels (rows are stored pixels).  plane > 0: y is the caller's NHWC tensor, its pixels `real` of `plane` stored ones.
@@ -154,7 +155,7 @@ struct LinearQ4Call {
   int plane = 0, real = 0;
   Epilogue ep;
 };
-LinearQ4Layout linear_q4_layout(int cin, int cout, int group, int scale_dtype, bool zeros);
+LinearQ4Layout linear_q4_layout(int cin, int cout, int group, int scale_dtype, bool zeros, int dtype);
 void linear_q4_pack(const LinearQ4Weights& w, const float* bias, uint8_t* blob);  // blob: layout.bytes bytes
 int launch_linear_q4(const LinearQ4Call& c, void* stream);
 

@@ -11,9 +11,11 @@
 //
 // x in 32 bits: a value is the exact sum of three bf16 numbers (8 + 8 + 8 digits), so a row of x becomes three columns of the product.
 //
-// Layout of the packed weights (host: linear_q4_pack): units of 16 outputs x 64 input channels, 512 bytes, lane l = 4 g + t of a
-// warp reads 16 of them: rows g and g + 8, channels 32 h + 8 t + 0 .. 7 of both halves h; the units of 16 outputs follow one
-// another along the input channels.  A lane's eight channels are contiguous in x, so x needs no rearrangement either.
+// Layout of the packed weights (linear_q4_pack): records of 16 outputs x 128 input channels, those of 16 outputs one after another.
+// A record is 1024 bytes of weights - lane l = 4 g + t of a warp reads bytes 16 l .. and 512 + 16 l .., which are rows g and g + 8,
+// channels 64 i + 32 h + 8 t + 0 .. 7 - and behind them the scales and zero points of the groups it touches ([group][8][2], rows g
+// and g + 8 side by side), so that one address leads to all that a lane needs and nothing is computed to find it.  A lane's eight
+// channels are contiguous in x too, so x needs no rearrangement.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -33,13 +35,15 @@ using namespace ptx;
 using namespace frag;
 
 constexpr int kWarps = 8, kThreads = kWarps * 32;
-// units of a block that a warp has in flight (with 32 columns there are registers for two only)
-int depth_of(int nt) { return nt == 4 ? 2 : 8; }
-constexpr int kUnitBytes = 512, kUnitK = 64;
-constexpr int kXBytes = 72 * 1024;        // most shared memory for staged rows of x: two CTAs on an SM, or three
+constexpr int kUnitK = 128, kUnitWeights = kUnitK * 16 / 2;
+// A warp's ring of copies: slots of two records (neighbours of one block, or one of each of two blocks).  Two CTAs of 8 warps keep
+// 128 KB of an SM's requests open.
+constexpr int kSlots = 4;
+constexpr int kSmemTwo = 113 * 1024;      // two CTAs on an SM
+constexpr int kSumBytes = 16000;          // most for the items' sums: with the rings (records of up to 1344 bytes) and one step of x inside that
 
 struct Params {
-  const unsigned char *wts, *scales, *zeros;
+  const unsigned char* wts;
   const float* bias;
   const void* x;
   const void* res;
@@ -47,54 +51,61 @@ struct Params {
   long long x_row, x_slice;   // elements between rows; between slices of 4 channels (0: channels are contiguous)
   long long y_row, y_slice;
   int rows, cin, cout;
-  int n_units, n_groups;      // units along the input channels; groups of a row
-  int scale_dtype;
-  unsigned mul_group;         // division by group / 32
-  int group32;
-  int tiles, kw, ks;          // tiles of output blocks; warps and CTAs that share a tile's sum
+  int n_units;                // records along the input channels
+  int tiles, kw, ks;          // tiles of output blocks, a cluster of ks CTAs each; parts of a block's sum in a CTA
   int row_tile, x_vec;
-  int chunk;                  // units of x staged at a time
+  int chunk;                  // records of x staged at a time
+  int ring_at, red_at;        // where the rings of copies, and the items' sums, begin in shared memory
+  unsigned low, high, digits; // masks of two weights of a word, and what they become the low digits of: as operands out of the
+                              // parameters (the compiler moves constants of this kind into registers again at every use)
   int act_pre, has_res, act_post;
   int plane, real;            // > 0: stored and real pixels of a plane, padding pixels are not written
 };
 
-__device__ __forceinline__ uint4 ldg_stream(const void* p) {
-  uint4 v;
-  asm volatile("ld.global.L1::no_allocate.L2::256B.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-  return v;
+__device__ __forceinline__ void copy16(unsigned dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// all but the last N groups of this thread's copies have landed
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], const unsigned (&a)[4], unsigned b0, unsigned b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// the same with the sum started from zero (as an operand: cleared registers cost four instructions more)
+__device__ __forceinline__ void mma_bf16z(float (&d)[4], const unsigned (&a)[4], unsigned b0, unsigned b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
+}
+template <bool BF, bool FIRST>
+__device__ __forceinline__ void mma(float (&d)[4], const unsigned (&a)[4], unsigned b0, unsigned b1) {
+  if (BF && FIRST) mma_bf16z(d, a, b0, b1);
+  else if (BF) mma_bf16(d, a, b0, b1);
+  else if (FIRST) mma16816z(d, a, b0, b1);
+  else mma16816(d, a, b0, b1);
+}
 
 // What is subtracted from the digits of a word's rows g and g + 8.
-template <bool BF>
 struct Zero {
   unsigned lo, hi;
 };
 template <bool BF>
-__device__ __forceinline__ Zero<BF> zero_of(unsigned z_lo, unsigned z_hi) {
-  Zero<BF> z;
-  if (BF) {
-    z.lo = 0x43004300u | z_lo * 0x10001u;          // 128 + z
-    z.hi = 0x43004300u | z_hi * 0x10001u;
-  } else {
-    z.lo = 0x64006400u | z_lo * 0x10001u;          // 1024 + z
-    z.hi = 0xd400d400u | z_hi * 0x100010u;         // -(64 + z)
-  }
-  return z;
+__device__ __forceinline__ Zero zero_of(const Params& p, unsigned z_lo, unsigned z_hi) {
+  if (BF) return Zero{p.digits | z_lo * 0x10001u, p.digits | z_hi * 0x10001u};  // 128 + z
+  return Zero{p.digits | z_lo * 0x10001u, 0xd400d400u | z_hi * 0x100010u};      // 1024 + z, -(64 + z)
 }
 
 // Eight weights of a word as the A operand: q - z, exact.
 template <bool BF>
-__device__ __forceinline__ void expand(unsigned w, const Zero<BF>& z, unsigned (&a)[4]) {
+__device__ __forceinline__ void expand(const Params& p, unsigned w, const Zero& z, unsigned (&a)[4]) {
   if (BF) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const unsigned v = ((w >> (4 * i)) & 0x000f000fu) | 0x43004300u;  // 128 + q
+      const unsigned v = ((w >> (4 * i)) & p.low) | p.digits;  // 128 + q
       const unsigned c = i & 1 ? z.hi : z.lo;
       const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v), *reinterpret_cast<const __nv_bfloat162*>(&c));
       a[i] = *reinterpret_cast<const unsigned*>(&d);
@@ -104,8 +115,8 @@ __device__ __forceinline__ void expand(unsigned w, const Zero<BF>& z, unsigned (
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const unsigned u = i ? w >> 8 : w;
-      const unsigned lo = (u & 0x000f000fu) | 0x64006400u;  // 1024 + q
-      const unsigned hi = (u & 0x00f000f0u) | 0x64006400u;  // 1024 + 16 q
+      const unsigned lo = (u & p.low) | p.digits;   // 1024 + q
+      const unsigned hi = (u & p.high) | p.digits;  // 1024 + 16 q
       const __half2 d0 = __hsub2(*reinterpret_cast<const __half2*>(&lo), *reinterpret_cast<const __half2*>(&z.lo));
       const __half2 d1 = __hfma2(*reinterpret_cast<const __half2*>(&hi), *reinterpret_cast<const __half2*>(&sixteenth),
                                  *reinterpret_cast<const __half2*>(&z.hi));
@@ -115,15 +126,22 @@ __device__ __forceinline__ void expand(unsigned w, const Zero<BF>& z, unsigned (
   }
 }
 
-// Scales of rows g and g + 8, neighbours in memory, as they are stored: converting them where they are loaded would wait for them.
-__device__ __forceinline__ uint2 load_scales(const Params& p, size_t at) {
-  if (p.scale_dtype == GI_F32) return *reinterpret_cast<const uint2*>(p.scales + at * 8);
-  return make_uint2(*reinterpret_cast<const unsigned*>(p.scales + at * 4), 0u);
+// Scales of rows g and g + 8.  S32: they are stored in 32 bits, else in the 16-bit type that x's kernel computes in (a choice by a
+// value of the call, among all three types, took 21 instructions of a record's 130).
+template <bool S32, bool BF>
+__device__ __forceinline__ float2 load_scales(unsigned at) {
+  if (S32) {
+    const uint2 v = lds64(at);
+    return make_float2(__uint_as_float(v.x), __uint_as_float(v.y));
+  }
+  const unsigned v = lds32(at);
+  if (BF) return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+  return __half22float2(*reinterpret_cast<const __half2*>(&v));
 }
-__device__ __forceinline__ float2 scales_f32(const Params& p, uint2 v) {
-  if (p.scale_dtype == GI_F32) return make_float2(__uint_as_float(v.x), __uint_as_float(v.y));
-  if (p.scale_dtype == GI_BF16) return make_float2(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u));
-  return __half22float2(*reinterpret_cast<const __half2*>(&v.x));
+__device__ __forceinline__ unsigned lds16(unsigned at) {
+  unsigned short v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at) : "memory");
+  return v;
 }
 
 // Eight channels k .. k + 7 of row r of x (16-bit types), zero behind the last one.
@@ -162,7 +180,7 @@ __device__ __forceinline__ void split3(float v, unsigned (&s)[3]) {
 // Rows of x for units [u0, u0 + n) into shared memory, `pitch` bytes a row.
 template <int XT>
 __device__ __forceinline__ void stage_x(const Params& p, unsigned char* xs, int pitch, int row0, int nrows, int u0, int n) {
-  const int per_row = n * 8;  // eights of channels
+  const int per_row = n * (kUnitK / 8);
   for (int i = threadIdx.x; i < per_row * nrows; i += kThreads) {
     const int r = i / per_row, c = i - r * per_row, k = u0 * kUnitK + c * 8;
     if (XT != GI_F32) {
@@ -188,9 +206,16 @@ __device__ __forceinline__ void stage_x(const Params& p, unsigned char* xs, int 
   }
 }
 
+// the activation; a NaN stays one
+__device__ __forceinline__ float act_nan(float v, int act) {
+  if (act != GI_ACT_NONE && v < 0.0f) v = 0.0f;
+  if (act == GI_ACT_RELU6 && v > 6.0f) v = 6.0f;
+  return v;
+}
+
 template <int XT>
 __device__ __forceinline__ void store_y(const Params& p, int r, int o, float v) {
-  v = act_f(v, p.act_pre);
+  v = act_nan(v, p.act_pre);
   long long at;
   if (p.y_slice) {
     at = (o >> 2) * p.y_slice + r * 4ll + (o & 3);
@@ -203,172 +228,233 @@ __device__ __forceinline__ void store_y(const Params& p, int r, int o, float v) 
     }
     at = row * p.y_row + o;
   }
-  if (p.has_res) v = act_f(v + __half2float(static_cast<const __half*>(p.res)[(o >> 2) * p.y_slice + r * 4ll + (o & 3)]), p.act_post);
+  if (p.has_res) v = act_nan(v + __half2float(static_cast<const __half*>(p.res)[(o >> 2) * p.y_slice + r * 4ll + (o & 3)]), p.act_post);
   if (XT == GI_F16) static_cast<__half*>(p.y)[at] = __float2half_rn(v);
   else if (XT == GI_BF16) static_cast<__nv_bfloat16*>(p.y)[at] = __float2bfloat16_rn(v);
   else static_cast<float*>(p.y)[at] = v;
 }
 
+// bytes of a record, of what lies in front of its zero points
+__host__ __device__ constexpr int zeros_at(int parts, bool wide) { return kUnitWeights + parts * 16 * (wide ? 4 : 2); }
+__host__ __device__ constexpr int record_bytes(int parts, bool wide, bool zeros) {
+  return (zeros_at(parts, wide) + (zeros ? parts * 16 : 0) + 31) / 32 * 32;  // whole sectors
+}
+
 // XT: type of x and y.  NT: eights of columns (rows of x, three for a row of 32 bits).  RB: blocks of 16 outputs of a warp.
-// G32: a group may end inside a unit.  ZP: zero points of the groups (else 8 everywhere).
-template <int XT, int NT, int RB, bool G32, bool ZP>
+// HG: groups that a record may touch, 1, 2 or 4 parts of it.  ZP: zero points of the groups (else 8 everywhere).  S32: scales in 32 bits.
+template <int XT, int NT, int RB, int HG, bool ZP, bool S32>
 __global__ void __launch_bounds__(kThreads, 2) linear_q4_kernel(const Params p) {
   extern __shared__ __align__(128) unsigned char smem[];
   constexpr bool BF = XT != GI_F16;
   constexpr int kCols = XT == GI_F32 ? 3 : 1;  // columns of a row of x
-  constexpr int HG = G32 ? 2 : 1;              // groups of a unit
-  constexpr int kDepth = NT == 4 ? 2 : 8;
+  constexpr int kZerosAt = zeros_at(HG, S32), kRecord = record_bytes(HG, S32, ZP), kBehind = kRecord - kUnitWeights;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int rank = blockIdx.x % p.ks, tile = blockIdx.x / p.ks % p.tiles, row0 = blockIdx.x / p.ks / p.tiles * p.row_tile;
   const int nrows = min(p.row_tile, p.rows - row0), cols = nrows * kCols;
-  const int kwi = warp % p.kw, blocks = (kWarps / p.kw) * RB;
-  const int n_blocks = (p.cout + 15) / 16;
-  const int block0 = tile * blocks + warp / p.kw * RB;  // this warp's blocks; those behind the last one are computed as the last
-  // this CTA's units, and how many of them this warp takes: kwi, kwi + kw, ...
+  const int n_blocks = (p.cout + 15) / 16, n_sets = (n_blocks + RB - 1) / RB;
+  // A tile's sets of RB blocks are cut into items: one set and one of kw parts of the CTA's share of the input channels.  Warp w
+  // takes the items w, w + 8, ..., one after the other; each leaves its sum in shared memory.
+  const int set0 = static_cast<int>(static_cast<long long>(n_sets) * tile / p.tiles), sets = static_cast<int>(static_cast<long long>(n_sets) * (tile + 1) / p.tiles) - set0;
+  const int items = sets * p.kw;
+  constexpr int kSteps = 2 / RB;  // records of a block that are one step
   const int ua = static_cast<int>(static_cast<long long>(p.n_units) * rank / p.ks), ub = static_cast<int>(static_cast<long long>(p.n_units) * (rank + 1) / p.ks);
-  const int mine = ub - ua > kwi ? (ub - ua - kwi + p.kw - 1) / p.kw : 0;
+  const int chunks = (ub - ua + p.chunk - 1) / p.chunk;
 
-  // units in flight: a slot is asked for again as soon as it has been used
-  uint4 w[RB][kDepth];
-  uint2 sc[RB][kDepth][HG];
-  unsigned zp[RB][kDepth][HG];
-  const unsigned char* wp[RB];
-  size_t gp[RB];
-#pragma unroll
-  for (int b = 0; b < RB; ++b) {
-    const size_t block = min(block0 + b, n_blocks - 1);
-    wp[b] = p.wts + (block * p.n_units + ua + kwi) * kUnitBytes + lane * 16;
-    gp[b] = block * p.n_groups * 8 + g;
-  }
-  auto load = [&](int j, int i) {
-    const int u = ua + kwi + i * p.kw;
-    size_t pair[HG];
-#pragma unroll
-    for (int h = 0; h < HG; ++h) {
-      const int half = 2 * u + h;
-      pair[h] = min(G32 && p.group32 == 1 ? half : div_by(half, p.mul_group), p.n_groups - 1) * 8;
-    }
-#pragma unroll
-    for (int b = 0; b < RB; ++b) {
-      w[b][j] = ldg_stream(wp[b] + static_cast<size_t>(i) * (p.kw * kUnitBytes));
-#pragma unroll
-      for (int h = 0; h < HG; ++h) {
-        sc[b][j][h] = load_scales(p, gp[b] + pair[h]);
-        if (ZP) zp[b][j][h] = *reinterpret_cast<const unsigned short*>(p.zeros + (gp[b] + pair[h]) * 2);
+  // This warp's own ring of copies.  (What else was tried: records held in registers, four loads deep - a warp tells its loads apart
+  // by six scoreboards and waits for all that share one; a copy of a whole record by one thread - some 90 instructions a record to
+  // ask and to wait for, where two records copied by every lane take 24 each.)
+  const unsigned xs = smem_u32(smem);
+  const unsigned ring = xs + p.ring_at + warp * (kSlots * 2) * kRecord;
+  // what is asked for next: `left` records of item a_item in chunk a_chunk, from `next` on
+  const unsigned char* next = nullptr;
+  size_t to_second = 0;
+  int a_item = warp - kWarps, a_chunk = 0, left = 0;
+  // records [first, last) of the CTA's share that item `item` has in chunk c: whole steps, but for the last of all
+  auto range = [&](int item, int c, int& first, int& last) {
+    const int part = item % p.kw, n = min(p.chunk, ub - ua - c * p.chunk), n_steps = (n + kSteps - 1) / kSteps;
+    first = c * p.chunk + n_steps * part / p.kw * kSteps;
+    last = c * p.chunk + min(n_steps * (part + 1) / p.kw * kSteps, n);
+  };
+  auto advance = [&] {  // to the next item that has records, if there is one
+    while (left <= 0 && a_chunk < chunks) {
+      a_item += kWarps;
+      if (a_item >= items) {
+        a_item = warp - kWarps;
+        ++a_chunk;
+        continue;
       }
+      int first, last;
+      range(a_item, a_chunk, first, last);
+      left = last - first;
+      const int block = (set0 + a_item / p.kw) * RB;
+      next = p.wts + (static_cast<size_t>(block) * p.n_units + ua + first) * kRecord + lane * 16;
+      if (RB == 2) to_second = block + 1 < n_blocks ? static_cast<size_t>(p.n_units) * kRecord : 0;  // (behind the last block: that one again)
     }
+  };
+  auto request = [&](unsigned slot) {
+    if (left > 0) {
+      const unsigned to = slot + lane * 16;
+      copy16(to, next);
+      copy16(to + 512, next + 512);
+      if (RB == 2) {
+        const unsigned char* other = next + to_second;
+        const unsigned to2 = to + kRecord;
+        copy16(to2, other);
+        copy16(to2 + 512, other + 512);
+        if (lane * 16 < kBehind) {
+          copy16(to + 1024, next + 1024);
+          copy16(to2 + 1024, other + 1024);
+        }
+      } else if (left > 1) {  // 2 x 1056 .. 1344 bytes
+        copy16(to + 1024, next + 1024);
+        copy16(to + 1536, next + 1536);
+        if (lane * 16 < 2 * kBehind) copy16(to + 2048, next + 2048);
+        if (512 < 2 * kBehind && 512 + lane * 16 < 2 * kBehind) copy16(to + 2560, next + 2560);
+      } else if (lane * 16 < kBehind) {
+        copy16(to + 1024, next + 1024);
+      }
+      next += kSteps * kRecord;
+      left -= kSteps;
+      if (left <= 0) advance();
+    }
+    copies_commit();
   };
 
   pdl_launch_dependents();
-  // What the first units bring is asked for while the kernel in front of this one ends: into L2 only, so that a blob that this very
-  // kernel's predecessor wrote is read as it left it.
-#pragma unroll
-  for (int j = 0; j < kDepth; ++j)
-    if (j < mine && (lane & 1) == 0) asm volatile("prefetch.global.L2 [%0];" ::"l"(wp[0] + static_cast<size_t>(j) * (p.kw * kUnitBytes)));
+  advance();
+  // What the first slots will hold is asked for while the kernel in front of this one ends: into L2 only, so that a blob that this
+  // very kernel's predecessor wrote is read as it left it.
+  if (lane == 0 && left > 0) {
+    const unsigned bytes = min(left, kSlots * kSteps) * kRecord;
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(next), "r"(bytes) : "memory");
+    if (RB == 2) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(next + to_second), "r"(bytes) : "memory");
+  }
   pdl_wait();
 #pragma unroll
-  for (int j = 0; j < kDepth; ++j)
-    if (j < mine) load(j, j);
+  for (int j = 0; j < kSlots; ++j) request(ring + j * 2 * kRecord);
 
   float acc[RB][NT][4];
-#pragma unroll
-  for (int b = 0; b < RB; ++b)
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) acc[b][n][i] = 0.0f;
-
   const int pitch = p.chunk * kUnitK * 2 + 64;  // 64 modulo 128: the eight columns of a fragment lie in different banks
-  const unsigned xs = smem_u32(smem);
+  // (lanes of columns that there are not read another's: a column of the product depends on its own column of x only)
+  unsigned col_at[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) col_at[n] = min(n * 8 + g, cols - 1) * pitch;
 
-  auto compute = [&](int j, unsigned at) {  // the unit in slot j; `at`: its channels of the first column of x
-    uint4 xb[NT][2];
+  auto compute = [&](const uint4 (&w)[RB][2], const float2 (&f)[RB][HG], const unsigned (&zp)[RB][HG], unsigned at) {
+    float part[RB][NT][4];
+    // a chain of products on one sum waits for each of them: with one column tile, two chains a record at least
+    constexpr int kChains = HG == 1 && NT == 1 ? 2 : HG;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const int col = n * 8 + g;
-      if (col < cols) {
-        xb[n][0] = lds128(at + col * pitch);
-        xb[n][1] = lds128(at + col * pitch + 64);
-      } else {
-        xb[n][0] = xb[n][1] = make_uint4(0u, 0u, 0u, 0u);
+    for (int i = 0; i < 2; ++i) {  // 64 channels
+      uint4 xb[NT][2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        xb[n][0] = lds128(at + col_at[n] + i * 128);
+        xb[n][1] = lds128(at + col_at[n] + i * 128 + 64);
       }
-    }
 #pragma unroll
-    for (int b = 0; b < RB; ++b) {
-      const unsigned word[4] = {w[b][j].x, w[b][j].y, w[b][j].z, w[b][j].w};
-      float part[NT][4];
+      for (int b = 0; b < RB; ++b) {
+        const unsigned word[4] = {w[b][i].x, w[b][i].y, w[b][i].z, w[b][i].w};
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const int h = G32 ? s >> 1 : 0;
-        const Zero<BF> z = ZP ? zero_of<BF>(zp[b][j][h] & 255u, zp[b][j][h] >> 8) : zero_of<BF>(8u, 8u);
-        unsigned a[4];
-        expand<BF>(word[s], z, a);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          const uint4& v = xb[n][s >> 1];
-          const unsigned b0 = s & 1 ? v.z : v.x, b1 = s & 1 ? v.w : v.y;
-          if (s == 0 || (G32 && s == 2)) part[n][0] = part[n][1] = part[n][2] = part[n][3] = 0.0f;
-          if (BF) mma_bf16(part[n], a, b0, b1);
-          else mma16816(part[n], a, b0, b1);
-        }
-        if (s == 3 || (G32 && s == 1)) {
-          const float2 f = scales_f32(p, sc[b][j][h]);
+        for (int s = 0; s < 4; ++s) {
+          const int q = 4 * i + s, h = q * HG / 8;  // 16 channels; their group
+          const bool first = q * kChains % 8 == 0, last = (q + 1) * kChains % 8 == 0;
+          const Zero z = ZP ? zero_of<BF>(p, zp[b][h] & 255u, zp[b][h] >> 8) : zero_of<BF>(p, 8u, 8u);
+          unsigned a[4];
+          expand<BF>(p, word[s], z, a);
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            acc[b][n][0] = fmaf(f.x, part[n][0], acc[b][n][0]);
-            acc[b][n][1] = fmaf(f.x, part[n][1], acc[b][n][1]);
-            acc[b][n][2] = fmaf(f.y, part[n][2], acc[b][n][2]);
-            acc[b][n][3] = fmaf(f.y, part[n][3], acc[b][n][3]);
+            const uint4& v = xb[n][s >> 1];
+            const unsigned b0 = s & 1 ? v.z : v.x, b1 = s & 1 ? v.w : v.y;
+            if (first) mma<BF, true>(part[b][n], a, b0, b1);
+            else mma<BF, false>(part[b][n], a, b0, b1);
+          }
+          if (last) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              acc[b][n][0] = fmaf(f[b][h].x, part[b][n][0], acc[b][n][0]);
+              acc[b][n][1] = fmaf(f[b][h].x, part[b][n][1], acc[b][n][1]);
+              acc[b][n][2] = fmaf(f[b][h].y, part[b][n][2], acc[b][n][2]);
+              acc[b][n][3] = fmaf(f[b][h].y, part[b][n][3], acc[b][n][3]);
+            }
           }
         }
       }
     }
   };
 
-  const int per_chunk = p.chunk / p.kw;  // units of a warp in a chunk: whole rounds of slots
-  for (int c = 0; c * p.chunk < ub - ua; ++c) {
+  // sums of the items: [item][block][column][16 outputs]
+  float* red = reinterpret_cast<float*>(smem + p.red_at);
+  unsigned from = ring;
+  for (int c = 0; c < chunks; ++c) {
     if (c) __syncthreads();  // every warp is done with the chunk before
     stage_x<XT>(p, smem, pitch, row0, nrows, ua + c * p.chunk, min(p.chunk, ub - ua - c * p.chunk));
     __syncthreads();
-    unsigned at = xs + kwi * (kUnitK * 2) + t * 16;
-    const int i1 = min((c + 1) * per_chunk, mine);
-    for (int i = c * per_chunk; i < i1; i += kDepth) {
+    for (int item = warp; item < items; item += kWarps) {
+      int first, last;
+      range(item, c, first, last);
 #pragma unroll
-      for (int j = 0; j < kDepth; ++j) {
-        if (i + j < i1) {
-          compute(j, at);
-          at += p.kw * (kUnitK * 2);
-          if (i + j + kDepth < mine) load(j, i + j + kDepth);
+      for (int b = 0; b < RB; ++b)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[b][n][j] = 0.0f;
+      unsigned at = xs + (first - c * p.chunk) * (kUnitK * 2) + t * 16;
+      for (int i = first; i < last; i += kSteps) {
+        copies_wait<kSlots - 1>();
+        __syncwarp();  // every lane's copies have
+        uint4 w[kSteps][RB][2];
+        float2 f[kSteps][RB][HG];
+        unsigned zp[kSteps][RB][HG];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int d = RB == 2 ? 0 : j, b = RB == 2 ? j : 0;
+          const unsigned rec = from + j * kRecord;
+          w[d][b][0] = lds128(rec + lane * 16);
+          w[d][b][1] = lds128(rec + lane * 16 + kUnitWeights / 2);
+#pragma unroll
+          for (int h = 0; h < HG; ++h) {
+            f[d][b][h] = load_scales<S32, BF>(rec + kUnitWeights + (h * 8 + g) * (S32 ? 8 : 4));
+            if (ZP) zp[d][b][h] = lds16(rec + kZerosAt + (h * 8 + g) * 2);
+          }
         }
+        __syncwarp();  // every lane has what it needs of the slot
+        request(from);
+        from = from == ring + (kSlots - 1) * 2 * kRecord ? ring : from + 2 * kRecord;
+        if (kSteps == 1 || i + 1 == last) {
+          compute(w[0], f[0], zp[0], at);
+        } else {
+          compute(w[0], f[0], zp[0], at);
+          compute(w[kSteps - 1], f[kSteps - 1], zp[kSteps - 1], at + kUnitK * 2);
+        }
+        at += kSteps * (kUnitK * 2);
       }
+#pragma unroll
+      for (int b = 0; b < RB; ++b)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int col = n * 8 + 2 * t + (j & 1);
+            float* to = red + ((item * RB + b) * cols + col) * 16 + g + (j >> 1) * 8;
+            if (col < cols) *to = c ? *to + acc[b][n][j] : acc[b][n][j];
+          }
     }
   }
 
-  // The warps' sums meet in shared memory, [warp][block][column][16 outputs], and are added in a fixed order.
-  __syncthreads();
-  float* red = reinterpret_cast<float*>(smem);
-#pragma unroll
-  for (int b = 0; b < RB; ++b)
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int col = n * 8 + 2 * t + (i & 1);
-        if (col < cols) red[((warp * RB + b) * (NT * 8) + col) * 16 + g + (i >> 1) * 8] = acc[b][n][i];
-      }
+  // The items' sums are added in a fixed order; the CTAs of a cluster share the outputs out among themselves.
   if (p.ks > 1) cluster_sync();
   else __syncthreads();
-  // the CTAs of a cluster share the outputs out among themselves
-  const int total = blocks * 16 * nrows;
+  const int outs = sets * RB * 16, total = outs * nrows;
   for (int i = threadIdx.x + rank * kThreads; i < total; i += kThreads * p.ks) {
-    const int r = i / (blocks * 16), ol = i - r * (blocks * 16), o = tile * blocks * 16 + ol;
+    const int r = i / outs, ol = i - r * outs, o = set0 * RB * 16 + ol;
     if (o >= p.cout) continue;
-    const int bl = ol >> 4, wr = bl / RB * p.kw;
+    const int bl = ol >> 4;
     float v = p.bias[o];
     for (int k = 0; k < p.ks; ++k) {
-      const unsigned base = p.ks > 1 ? mapa_shared(xs, k) : 0u;
+      const unsigned base = p.ks > 1 ? mapa_shared(xs + p.red_at, k) : 0u;
       for (int j = 0; j < p.kw; ++j) {
-        const int at = (((wr + j) * RB + bl % RB) * (NT * 8) + r * kCols) * 16 + (ol & 15);
+        const int at = (((bl / RB * p.kw + j) * RB + bl % RB) * cols + r * kCols) * 16 + (ol & 15);
 #pragma unroll
         for (int c = 0; c < kCols; ++c) {
           if (p.ks > 1) {
@@ -386,15 +472,18 @@ __global__ void __launch_bounds__(kThreads, 2) linear_q4_kernel(const Params p) 
   if (p.ks > 1) cluster_sync();  // nobody leaves while its shared memory is read
 }
 
-template <int XT, int NT, int RB>
-cudaError_t launch_shape(const Params& p, bool zeros, unsigned grid, size_t smem, cudaStream_t stream) {
-  const bool g32 = p.group32 % 2 != 0;
-  void (*k)(const Params) = g32 ? (zeros ? linear_q4_kernel<XT, NT, RB, true, true> : linear_q4_kernel<XT, NT, RB, true, false>)
-                                : (zeros ? linear_q4_kernel<XT, NT, RB, false, true> : linear_q4_kernel<XT, NT, RB, false, false>);
-  static bool raised[2][2][kMaxDevices] = {};
-  bool& done = raised[g32][zeros][current_device_slot()];
+// parts of a record that may belong to different groups
+int parts_of(int group) { return group % 128 == 0 ? 1 : group % 64 == 0 ? 2 : 4; }
+
+template <int XT, int NT, int RB, bool S32>
+cudaError_t launch_shape(const Params& p, int parts, bool zeros, unsigned grid, size_t smem, cudaStream_t stream) {
+  void (*k)(const Params) = parts == 1   ? (zeros ? linear_q4_kernel<XT, NT, RB, 1, true, S32> : linear_q4_kernel<XT, NT, RB, 1, false, S32>)
+                            : parts == 2 ? (zeros ? linear_q4_kernel<XT, NT, RB, 2, true, S32> : linear_q4_kernel<XT, NT, RB, 2, false, S32>)
+                                         : (zeros ? linear_q4_kernel<XT, NT, RB, 4, true, S32> : linear_q4_kernel<XT, NT, RB, 4, false, S32>);
+  static bool raised[3][2][kMaxDevices] = {};
+  bool& done = raised[parts / 2][zeros][current_device_slot()];
   if (!done) {
-    const cudaError_t err = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kXBytes);
+    const cudaError_t err = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemTwo);
     if (err != cudaSuccess) return err;
     done = true;
   }
@@ -415,97 +504,126 @@ cudaError_t launch_shape(const Params& p, bool zeros, unsigned grid, size_t smem
 }
 
 struct Shape {
-  int nt, rb, kw, ks, row_tile;
+  int nt, rb, tiles, kw, ks, row_tile;
 };
 
-// Which shape of the kernel runs a product: columns a CTA takes at once, warps (kw) and CTAs (ks) that share an output's sum.
+// Which shape of the kernel runs a product: columns a CTA takes at once, tiles of outputs, CTAs (ks) that share a tile's sums and
+// parts (kw) of a CTA's share of a sum.
 Shape choose_shape(int rows, int cols_per_row, int n_blocks, int n_units, int sms) {
   Shape s{};
   const int fit = 32 / cols_per_row;
   s.row_tile = std::min(rows, fit);
   const int cols = s.row_tile * cols_per_row;
   s.nt = cols <= 8 ? 1 : cols <= 16 ? 2 : 4;
-  s.rb = s.nt == 4 ? 2 : 1;
-  s.kw = 8;
-  while (s.kw > 1 && s.kw * cols > 64) s.kw /= 2;
-  while (s.kw > 1 && s.kw * depth_of(s.nt) > 2 * n_units) s.kw /= 2;
-  const int tiles = (n_blocks + kWarps / s.kw * s.rb - 1) / (kWarps / s.kw * s.rb);
-  const long long ctas = static_cast<long long>(tiles) * ((rows + s.row_tile - 1) / s.row_tile);
-  s.ks = 1;
-  while (s.ks < 8 && ctas * s.ks * 2 <= 2 * sms && s.ks * s.kw * depth_of(s.nt) <= n_units) s.ks *= 2;
+  s.rb = s.nt == 1 ? 1 : 2;
+  const int n_sets = (n_blocks + s.rb - 1) / s.rb;
+  // Two CTAs an SM.  Several rows: pairs of CTAs share x out among themselves, each stages half of its channels (8 rows 4096 -> 12288
+  // 15.1 us, alone 17.0; one row 8192 -> 28672 32.5 and 32.6).  Few outputs of many channels: more CTAs share a sum, as long as each
+  // has 2048 channels of it (4 rows 16384 -> 512: 8 CTAs 7.5 us, 4 7.6, 1 35; one row 1280 -> 1001: 1 CTA 3.0 us, 2 3.5).
+  s.ks = cols >= 4 && n_sets >= sms && n_units >= 2 ? 2 : 1;
+  s.tiles = std::min(n_sets, 2 * sms / s.ks);
+  while (s.ks < 8 && s.tiles * s.ks * 2 <= sms && n_units >= 32 * s.ks) s.ks *= 2;
+  // an item for each warp, of a step or more
+  s.kw = 1;
+  auto sets = [&] { return (n_sets + s.tiles - 1) / s.tiles; };
+  while (s.kw < 8 && sets() * s.kw < kWarps && s.kw * s.ks * 2 <= n_units) s.kw *= 2;
+  const int part = s.rb * cols * 16 * 4;  // bytes of an item's sum
+  while (s.kw > 1 && sets() * s.kw * part > kSumBytes) s.kw /= 2;
+  if (sets() * part > kSumBytes) {
+    const int most = kSumBytes / part;
+    s.tiles = (n_sets + most - 1) / most;
+  }
   return s;
 }
 
-template <int XT>
-cudaError_t launch_type(const Params& p, const Shape& s, bool zeros, unsigned grid, size_t smem, cudaStream_t stream) {
+template <int XT, bool S32>
+cudaError_t launch_type(const Params& p, const Shape& s, int parts, bool zeros, unsigned grid, size_t smem, cudaStream_t stream) {
   switch (s.nt) {
-    case 1: return launch_shape<XT, 1, 1>(p, zeros, grid, smem, stream);
-    case 2: return launch_shape<XT, 2, 1>(p, zeros, grid, smem, stream);
-    default: return launch_shape<XT, 4, 2>(p, zeros, grid, smem, stream);
+    case 1: return launch_shape<XT, 1, 1, S32>(p, parts, zeros, grid, smem, stream);
+    case 2: return launch_shape<XT, 2, 2, S32>(p, parts, zeros, grid, smem, stream);
+    default: return launch_shape<XT, 4, 2, S32>(p, parts, zeros, grid, smem, stream);
   }
 }
+
+// Whether a layer's packed scales are 32 bits wide: those of 16 bits are kept where they are of the type its kernel computes in.
+bool wide_scales(int scale_dtype, int dtype) { return scale_dtype != (dtype == GI_F16 ? GI_F16 : GI_BF16); }
 
 int scale_bytes(int dtype) { return dtype == GI_F32 ? 4 : 2; }
 
 }  // namespace
 
-LinearQ4Layout linear_q4_layout(int cin, int cout, int group, int scale_dtype, bool zeros) {
+LinearQ4Layout linear_q4_layout(int cin, int cout, int group, int scale_dtype, bool zeros, int dtype) {
   LinearQ4Layout l;
   l.n_blocks = (cout + 15) / 16;
   l.n_units = (cin + kUnitK - 1) / kUnitK;
-  l.n_groups = static_cast<int>((static_cast<int64_t>(cin) + group - 1) / group);
-  const uint64_t per_group = static_cast<uint64_t>(l.n_blocks) * l.n_groups * 16;
-  l.scales = round_up_u64(static_cast<uint64_t>(l.n_blocks) * l.n_units * kUnitBytes, 256);
-  l.zeros = round_up_u64(l.scales + per_group * scale_bytes(scale_dtype), 256);
-  l.bias = round_up_u64(l.zeros + (zeros ? per_group : 0), 256);
+  l.parts = parts_of(group);
+  l.zeros_at = zeros_at(l.parts, wide_scales(scale_dtype, dtype));
+  l.record = record_bytes(l.parts, wide_scales(scale_dtype, dtype), zeros);
+  l.bias = round_up_u64(static_cast<uint64_t>(l.n_blocks) * l.n_units * l.record, 256);
   l.bytes = round_up_u64(l.bias + static_cast<uint64_t>(l.n_blocks) * 16 * sizeof(float), 256);
   return l;
 }
 
 void linear_q4_pack(const LinearQ4Weights& w, const float* bias, uint8_t* blob) {
-  const LinearQ4Layout l = linear_q4_layout(w.cin, w.cout, w.group, w.scale_dtype, w.zeros != nullptr);
-  std::memset(blob, 0, l.bytes);
+  const LinearQ4Layout l = linear_q4_layout(w.cin, w.cout, w.group, w.scale_dtype, w.zeros != nullptr, w.dtype);
   const int64_t pitch = (static_cast<int64_t>(w.cin) + 1) / 2;  // bytes of a row of the caller's
-  uint32_t* out = reinterpret_cast<uint32_t*>(blob);
+  const int64_t n_groups = (static_cast<int64_t>(w.cin) + w.group - 1) / w.group;
+  const int sb = scale_bytes(w.scale_dtype);
+  const bool wide = wide_scales(w.scale_dtype, w.dtype);
   for (int b = 0; b < l.n_blocks; ++b)
-    for (int u = 0; u < l.n_units; ++u)
+    for (int u = 0; u < l.n_units; ++u) {
+      // zero behind the last channel and the last output: x is staged as zeros there, such outputs are not stored
+      uint8_t* rec = blob + (static_cast<size_t>(b) * l.n_units + u) * l.record;
+      std::memset(rec + kUnitWeights, 0, l.record - kUnitWeights);
+      uint32_t words[kUnitWeights / 4];
       for (int g = 0; g < 8; ++g) {
-        // two rows' 32 bytes of this unit, zero behind the last channel and the last output
         uint8_t row[2][kUnitK / 2] = {};
         for (int i = 0; i < 2; ++i) {
           const int o = b * 16 + g + 8 * i;
+          if (o >= w.cout) continue;
           const int64_t at = static_cast<int64_t>(u) * (kUnitK / 2), n = std::min<int64_t>(kUnitK / 2, pitch - at);
-          if (o < w.cout) std::memcpy(row[i], w.q + o * pitch + at, static_cast<size_t>(n));
-        }
-        for (int t = 0; t < 4; ++t)
-          for (int s = 0; s < 4; ++s) {
-            const int at = (s >> 1) * 16 + t * 4 + (s & 1) * 2;  // byte of channel 32 (s / 2) + 8 t + 4 (s % 2)
-            const uint32_t a0 = row[0][at], a1 = row[0][at + 1], c0 = row[1][at], c1 = row[1][at + 1];
-            out[((static_cast<size_t>(b) * l.n_units + u) * 32 + g * 4 + t) * 4 + s] =
-                (a0 & 15u) | (c0 & 15u) << 4 | (a1 & 15u) << 8 | (c1 & 15u) << 12 | (a0 >> 4) << 16 | (c0 >> 4) << 20 | (a1 >> 4) << 24 | (c1 >> 4) << 28;
+          std::memcpy(row[i], w.q + o * pitch + at, static_cast<size_t>(n));
+          for (int h = 0; h < l.parts; ++h) {
+            const int64_t gr = std::min<int64_t>((static_cast<int64_t>(u) * kUnitK + h * (kUnitK / l.parts)) / w.group, n_groups - 1);
+            const size_t from = static_cast<size_t>(o) * n_groups + gr, to = h * 16 + g * 2 + i;
+            const uint8_t* scale = static_cast<const uint8_t*>(w.scales) + from * sb;
+            if (wide && sb == 2) {
+              uint16_t v;
+              std::memcpy(&v, scale, 2);
+              const float f = w.scale_dtype == GI_F16 ? f16_to_f32(v) : bf16_to_f32(v);
+              std::memcpy(rec + kUnitWeights + to * 4, &f, 4);
+            } else {
+              std::memcpy(rec + kUnitWeights + to * sb, scale, sb);
+            }
+            if (w.zeros) rec[l.zeros_at + to] = w.zeros[from] & 15u;
           }
+        }
+        for (int i = 0; i < 2; ++i)
+          for (int t = 0; t < 4; ++t)
+            for (int s = 0; s < 4; ++s) {
+              const int at = i * 32 + (s >> 1) * 16 + t * 4 + (s & 1) * 2;  // byte of channel 64 i + 32 (s / 2) + 8 t + 4 (s % 2)
+              const uint32_t a0 = row[0][at], a1 = row[0][at + 1], c0 = row[1][at], c1 = row[1][at + 1];
+              words[(i * 32 + g * 4 + t) * 4 + s] = (a0 & 15u) | (c0 & 15u) << 4 | (a1 & 15u) << 8 | (c1 & 15u) << 12 | (a0 >> 4) << 16 |
+                                                    (c0 >> 4) << 20 | (a1 >> 4) << 24 | (c1 >> 4) << 28;
+            }
       }
-  // scales and zero points: [block of 16 outputs][group][8][2], outputs g and g + 8 side by side
-  const int sb = scale_bytes(w.scale_dtype);
-  for (int o = 0; o < w.cout; ++o)
-    for (int gr = 0; gr < l.n_groups; ++gr) {
-      const size_t to = (static_cast<size_t>(o / 16) * l.n_groups + gr) * 16 + (o % 8) * 2 + o % 16 / 8, from = static_cast<size_t>(o) * l.n_groups + gr;
-      std::memcpy(blob + l.scales + to * sb, static_cast<const uint8_t*>(w.scales) + from * sb, sb);
-      if (w.zeros) blob[l.zeros + to] = w.zeros[from] & 15u;
+      std::memcpy(rec, words, sizeof words);
     }
+  std::memset(blob + l.bias, 0, l.bytes - l.bias);
   if (bias) std::memcpy(blob + l.bias, bias, static_cast<size_t>(w.cout) * sizeof(float));
 }
 
 int launch_linear_q4(const LinearQ4Call& c, void* stream) {
   if (c.rows <= 0) return 0;
-  const LinearQ4Layout l = linear_q4_layout(c.cin, c.cout, c.group, c.scale_dtype, c.zeros);
+  const LinearQ4Layout l = linear_q4_layout(c.cin, c.cout, c.group, c.scale_dtype, c.zeros, c.dtype);
   const int cols_per_row = c.dtype == GI_F32 ? 3 : 1;
   const Shape s = choose_shape(c.rows, cols_per_row, l.n_blocks, l.n_units, device_sm_count());
   Params p{};
   const unsigned char* blob = static_cast<const unsigned char*>(c.blob);
   p.wts = blob;
-  p.scales = blob + l.scales;
-  p.zeros = blob + l.zeros;
+  p.low = 0x000f000fu;
+  p.high = 0x00f000f0u;
+  p.digits = c.dtype == GI_F16 ? 0x64006400u : 0x43004300u;
   p.bias = reinterpret_cast<const float*>(blob + l.bias);
   p.x = c.x;
   p.res = c.res;
@@ -518,36 +636,42 @@ int launch_linear_q4(const LinearQ4Call& c, void* stream) {
   p.cin = c.cin;
   p.cout = c.cout;
   p.n_units = l.n_units;
-  p.n_groups = l.n_groups;
-  p.scale_dtype = c.scale_dtype;
-  p.group32 = std::min(c.group / 32, 2 * l.n_units);  // one group: as many halves of units as there are
-  p.mul_group = p.group32 > 1 ? magic(static_cast<uint64_t>(p.group32)) : 0u;
   p.kw = s.kw;
   p.ks = s.ks;
   p.row_tile = s.row_tile;
-  const int blocks = kWarps / s.kw * s.rb, elem = c.dtype == GI_F32 ? 4 : 2, cols = s.row_tile * cols_per_row;
-  p.tiles = (l.n_blocks + blocks - 1) / blocks;
+  const int elem = c.dtype == GI_F32 ? 4 : 2, cols = s.row_tile * cols_per_row;
+  p.tiles = s.tiles;
   p.x_vec = c.x_slice == 0 && reinterpret_cast<uintptr_t>(c.x) % 16 == 0 && (c.rows == 1 || c.x_row * elem % 16 == 0);
-  // units staged at a time: whole rounds of slots of every warp
-  const int step = s.kw * depth_of(s.nt);
-  const int fit = (kXBytes / cols - 64) / (kUnitK * 2);
-  const int need = (l.n_units + s.ks - 1) / s.ks;
-  p.chunk = std::max(step, std::min(fit / step * step, (need + step - 1) / step * step));
+  // shared memory: x (as much of it as two CTAs on an SM leave room for), the rings of copies, the items' sums
+  const int n_sets = (l.n_blocks + s.rb - 1) / s.rb, sets = (n_sets + s.tiles - 1) / s.tiles;
+  const int rings = kWarps * kSlots * 2 * l.record, sums = sets * s.kw * s.rb * cols * 16 * 4;
+  const int fit = ((kSmemTwo - rings - sums) / cols - 64) / (kUnitK * 2);
+  const int need = (l.n_units + s.ks - 1) / s.ks, step = 2 / s.rb;
+  p.chunk = std::max(1, std::min(fit / step, (need + step - 1) / step)) * step;
+  p.ring_at = (cols * (p.chunk * kUnitK * 2 + 64) + 127) / 128 * 128;
+  p.red_at = p.ring_at + rings;
   p.act_pre = c.ep.act_pre;
   p.has_res = c.ep.has_res;
   p.act_post = c.ep.act_post;
   p.plane = c.plane;
   p.real = c.real;
-  const size_t smem = std::max<size_t>(static_cast<size_t>(cols) * (p.chunk * kUnitK * 2 + 64), static_cast<size_t>(kWarps) * s.rb * s.nt * 8 * 16 * 4);
+  const size_t smem = static_cast<size_t>(p.red_at) + sums;
   const long long grid = static_cast<long long>(p.tiles) * s.ks * ((c.rows + s.row_tile - 1) / s.row_tile);
-  if (grid > 0x7fffffffll || smem > kXBytes) return static_cast<int>(cudaErrorInvalidConfiguration);
+  if (grid > 0x7fffffffll || smem > kSmemTwo) return static_cast<int>(cudaErrorInvalidConfiguration);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const unsigned n = static_cast<unsigned>(grid);
-  switch (c.dtype) {
-    case GI_F16: return static_cast<int>(launch_type<GI_F16>(p, s, c.zeros, n, smem, st));
-    case GI_BF16: return static_cast<int>(launch_type<GI_BF16>(p, s, c.zeros, n, smem, st));
-    default: return static_cast<int>(launch_type<GI_F32>(p, s, c.zeros, n, smem, st));
+  const int parts = parts_of(c.group);
+  cudaError_t err;
+  if (wide_scales(c.scale_dtype, c.dtype)) {
+    err = c.dtype == GI_F16    ? launch_type<GI_F16, true>(p, s, parts, c.zeros, n, smem, st)
+          : c.dtype == GI_BF16 ? launch_type<GI_BF16, true>(p, s, parts, c.zeros, n, smem, st)
+                               : launch_type<GI_F32, true>(p, s, parts, c.zeros, n, smem, st);
+  } else {
+    err = c.dtype == GI_F16    ? launch_type<GI_F16, false>(p, s, parts, c.zeros, n, smem, st)
+          : c.dtype == GI_BF16 ? launch_type<GI_BF16, false>(p, s, parts, c.zeros, n, smem, st)
+                               : launch_type<GI_F32, false>(p, s, parts, c.zeros, n, smem, st);
   }
+  return static_cast<int>(err);
 }
 
 }  // namespace gi

@@ -31,27 +31,37 @@ def make(seed, cin, cout, group, dtype, scale=torch.float16, zeros=False, bias=T
 
 
 # ---------------------------------------------------------------- host
-def unpack_blob(blob, cin, cout, group, scale_bytes, zeros):
-    """q, scale bytes and zero points out of a packed blob: the layout that the kernel's comment states, restated."""
-    nb, nu, ng = -(-cout // 16), -(-cin // 64), -(-cin // group)
-    up = lambda v: -(-v // 256) * 256  # noqa: E731
-    words = blob[:nb * nu * 512].view(np.uint32).reshape(nb, nu, 8, 4, 4)  # block, unit, g, t, word
-    q = np.zeros((nb * 16, nu * 64), dtype=np.uint8)
-    for s in range(4):
-        for nib in range(8):
-            row, off = nib % 2, 2 * (nib % 4 // 2) + nib // 4  # row g or g + 8; channel within four
-            v = (words[..., s] >> (4 * nib)) & 15
-            for t in range(4):
-                k = 32 * (s // 2) + 8 * t + 4 * (s % 2) + off
-                q.reshape(nb, 2, 8, nu, 64)[:, row, :, :, k] = v[..., t].transpose(0, 2, 1)
-    at = up(nb * nu * 512)
-    pairs = lambda a, n: a.reshape(nb, ng, 8, 2, n).transpose(0, 3, 2, 1, 4).reshape(nb * 16, ng, n)[:cout]  # noqa: E731
-    sc = pairs(blob[at:at + nb * ng * 16 * scale_bytes], scale_bytes)
-    at = up(at + nb * ng * 16 * scale_bytes)
-    z = pairs(blob[at:at + nb * ng * 16], 1)[..., 0] if zeros else None
-    at = up(at + (nb * ng * 16 if zeros else 0))
+def unpack_blob(blob, cin, cout, group, sb, zeros):
+    """q, scale bytes, zero points and bias out of a packed blob: the layout that the kernel's comment states, restated.  sb: bytes
+    of a scale."""
+    nb, nu, ng = -(-cout // 16), -(-cin // 128), -(-cin // group)
+    parts = 1 if group % 128 == 0 else 2 if group % 64 == 0 else 4
+    zat = 1024 + parts * 16 * sb
+    record = -(-(zat + (parts * 16 if zeros else 0)) // 32) * 32
+    recs = blob[:nb * nu * record].reshape(nb, nu, record)
+    words = np.ascontiguousarray(recs[..., :1024]).view(np.uint32).reshape(nb, nu, 2, 8, 4, 4)  # block, unit, half, g, t, word
+    q = np.zeros((nb, 2, 8, nu, 128), dtype=np.uint8)
+    for half in range(2):
+        for s in range(4):
+            for nib in range(8):
+                row, off = nib % 2, 2 * (nib % 4 // 2) + nib // 4  # row g or g + 8; channel within four
+                v = (words[:, :, half, :, :, s] >> (4 * nib)) & 15
+                for t in range(4):
+                    k = 64 * half + 32 * (s // 2) + 8 * t + 4 * (s % 2) + off
+                    q[:, row, :, :, k] = v[..., t].transpose(0, 2, 1)
+    sc, z = np.zeros((nb * 16, ng, sb), dtype=np.uint8), np.zeros((nb * 16, ng), dtype=np.uint8)
+    for u in range(nu):
+        for h in range(parts):
+            gr = (u * 128 + h * (128 // parts)) // group
+            if gr >= ng:
+                continue
+            at = 1024 + h * 16 * sb
+            sc.reshape(nb, 2, 8, ng, sb)[:, :, :, gr] = recs[:, u, at:at + 16 * sb].reshape(nb, 8, 2, sb).transpose(0, 2, 1, 3)
+            if zeros:
+                z.reshape(nb, 2, 8, ng)[:, :, :, gr] = recs[:, u, zat + h * 16:zat + h * 16 + 16].reshape(nb, 8, 2).transpose(0, 2, 1)
+    at = -(-nb * nu * record // 256) * 256
     bias = blob[at:at + nb * 64].view(np.float32)[:cout]
-    return q[:cout, :cin], sc, z, bias
+    return q.reshape(nb * 16, nu * 128)[:cout, :cin], sc[:cout], z[:cout], bias
 
 
 @pytest.mark.parametrize("cin,cout,group,scale,zeros", [(64, 16, 32, torch.float16, False), (1, 1, 32, torch.float32, True), (97, 33, 32, torch.float16, True),
@@ -59,6 +69,8 @@ def unpack_blob(blob, cin, cout, group, scale_bytes, zeros):
 def test_pack_keeps_every_value_in_its_place(cin, cout, group, scale, zeros):
     layer, (q, s, z, b) = make(3, cin, cout, group, torch.float16, scale, zeros, device="cpu")
     sb = s.element_size()
+    if scale == torch.bfloat16:  # kept in 32 bits beside rows of fp16
+        s, sb = s.float(), 4
     got_q, got_s, got_z, got_b = unpack_blob(layer.blob.numpy(), cin, cout, group, sb, zeros)
     assert np.array_equal(got_q, torch.stack([q & 15, q >> 4], -1).flatten(1)[:, :cin].numpy())
     assert np.array_equal(got_s, s.view(torch.uint8).reshape(cout, -1, sb).numpy())
