@@ -408,6 +408,29 @@ GI_API gi_status gi_linear_q4_pack(const gi_linear_q4* layer, const uint8_t* q, 
 GI_API gi_status gi_linear_q4_run(const gi_linear_q4* layer, const void* dev_blob, const void* dev_x, int64_t ldx, void* dev_y, int64_t ldy,
                                   int32_t rows, void* stream);
 
+/* What rows of logits say.  With p = softmax(logits / temperature) of a row, fp32 results:
+ *   given_log_probs[r,j] = log p[given[r,j]]    (0 for a negative class: nothing asked; NaN for one >= classes)
+ *   entropy[r]           = - sum p log p        (natural logarithm)
+ *   top_ids[r,j], top_log_probs[r,j]            the `top` most probable classes, the most probable first, of equals the lower class
+ * Logits may be minus infinity (a class excluded): such classes have probability 0 and log probability minus infinity, and come last
+ * in the order of their numbers.  A row of nothing else has entropy 0.  A NaN or plus infinity makes a row's fp32 results NaN (a NaN
+ * leads the order); other rows are not affected.  Sums are fp32, relative to the row's maximum.
+ * (Classification and segmentation networks end in such rows: NHWC logits are [batch * H * W][classes].) */
+#define GI_MAX_TOP 32
+typedef struct gi_log_probs_desc {
+  int32_t rows;           /* >= 0, up to 2^28 */
+  int32_t classes;        /* up to 2^24 */
+  int64_t ld;             /* elements between rows, >= classes (not looked at for rows <= 1) */
+  int32_t dtype;          /* of the logits: GI_F16, GI_BF16 or GI_F32 */
+  float temperature;      /* 1e-4 .. 1e4 */
+  int32_t n_given;        /* classes asked for in each row, 0 .. 65536 */
+  int32_t top;            /* 0 .. GI_MAX_TOP, at most `classes` */
+} gi_log_probs_desc;
+
+/* dev_given [rows][n_given] and the outputs are contiguous; those of 0 columns may be NULL, and so may dev_entropy. */
+GI_API gi_status gi_log_probs(const gi_log_probs_desc* desc, const void* dev_logits, const int32_t* dev_given, float* dev_given_log_probs,
+                              float* dev_entropy, int32_t* dev_top_ids, float* dev_top_log_probs, void* stream);
+
 GI_API void gi_exec_destroy(gi_exec* e);
 
 /* ---- helpers ---- */

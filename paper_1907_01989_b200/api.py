@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import List, Optional, Sequence
+from typing import Any, List, NamedTuple, Optional, Sequence
 
 import numpy as np
 
@@ -29,6 +29,7 @@ GI_PLAN_GREEDY_BY_SIZE, GI_PLAN_GREEDY_SHARED_OBJECTS, GI_PLAN_NAIVE, GI_PLAN_MI
 GI_PW_AUTO, GI_PW_SIMT, GI_PW_TC_PAIR, GI_PW_TC_LANE, GI_PW_TC_WIDE, GI_PW_RULE = 0, 1, 2, 3, 4, 5
 GI_XOP_AUTO, GI_XOP_OFF, GI_XOP_ON, GI_XOP_CHAIN = 0, 1, 2, 3
 GI_STATIC_ARENA_BYTES = 16 << 20
+GI_MAX_TOP = 32
 KERNEL_NAMES = {1: "pack", 2: "unpack", 3: "conv_simt", 4: "pointwise_tc", 5: "depthwise", 6: "eltwise", 7: "pool",
                 8: "resize", 9: "conv3x3_tc", 10: "pointwise_ts", 11: "depthwise_pointwise", 12: "none", 13: "concat", 14: "conv_tc", 15: "inverted_residual", 16: "pointwise_mm", 17: "pointwise_chain", 18: "block_mma", 19: "pointwise_mma", 20: "conv_mma"}
 
@@ -78,10 +79,15 @@ class gi_linear_q4(C.Structure):
                 ("dtype", C.c_int32), ("act", C.c_int32)]
 
 
+class gi_log_probs_desc(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("classes", C.c_int32), ("ld", C.c_int64), ("dtype", C.c_int32), ("temperature", C.c_float),
+                ("n_given", C.c_int32), ("top", C.c_int32)]
+
+
 EXPORTS = ["gi_graph_create", "gi_graph_input", "gi_add_op", "gi_graph_output", "gi_graph_destroy", "gi_compile",
            "gi_exec_query", "gi_exec_tensor", "gi_exec_op", "gi_exec_launch", "gi_exec_bind", "gi_run", "gi_run_static", "gi_run_timed", "gi_device_status", "gi_selftest_bounded_wait", "gi_exec_destroy",
            "gi_slice8_tensor_bytes", "gi_slice8_pointwise_blob_bytes", "gi_slice8_pointwise_pack", "gi_slice8_pointwise_run",
-           "gi_linear_q4_blob_bytes", "gi_linear_q4_pack", "gi_linear_q4_run",
+           "gi_linear_q4_blob_bytes", "gi_linear_q4_pack", "gi_linear_q4_run", "gi_log_probs",
            "gi_status_str", "gi_last_error", "gi_tensor_bytes", "gi_f32_to_f16"]
 
 _lib = None
@@ -140,6 +146,8 @@ def lib() -> C.CDLL:
     L.gi_linear_q4_pack.restype = C.c_int32
     L.gi_linear_q4_run.argtypes = [C.POINTER(gi_linear_q4), vp, vp, C.c_int64, vp, C.c_int64, C.c_int32, vp]
     L.gi_linear_q4_run.restype = C.c_int32
+    L.gi_log_probs.argtypes = [C.POINTER(gi_log_probs_desc)] + [vp] * 7
+    L.gi_log_probs.restype = C.c_int32
     L.gi_status_str.argtypes = [C.c_int32]
     L.gi_status_str.restype = C.c_char_p
     L.gi_last_error.argtypes = []
@@ -289,6 +297,51 @@ class LinearQ4:
             raise ValueError(f"x has {rows} rows, y {yrows}")
         _check(_on(self.device, stream, lambda s: lib().gi_linear_q4_run(self._ref, self.blob.data_ptr(), xp, ldx, yp, ldy, rows, s)), "gi_linear_q4_run")
         return y
+
+
+class LogProbs(NamedTuple):
+    """Results of log_probs for rows of logits; None where nothing was asked for."""
+    given: Any     # [rows, n] float32: log probabilities of the given classes
+    entropy: Any   # [rows] float32
+    top: Any       # [rows, top] float32: log probabilities of the most probable classes, the most probable first
+    top_ids: Any   # [rows, top] int32: these classes
+
+
+def log_probs_out(rows: int, n_given: int = 0, top: int = 0, device="cuda:0", entropy: bool = True) -> LogProbs:
+    """Result buffers for log_probs."""
+    import torch
+
+    def new(n, dtype):
+        return torch.empty((rows, n), dtype=dtype, device=device) if n else None
+    return LogProbs(new(n_given, torch.float32), torch.empty((rows,), dtype=torch.float32, device=device) if entropy else None,
+                    new(top, torch.float32), new(top, torch.int32))
+
+
+def log_probs(logits, given=None, top: int = 0, temperature: float = 1.0, out: Optional[LogProbs] = None, stream=None) -> LogProbs:
+    """gi_log_probs: logits [..., classes] (float16, bfloat16, float32; two axes may have any distance between rows, other tensors are
+    contiguous) -> log probabilities of `given` (int32 [..., n], negative: nothing asked), entropy and the `top` leading classes of
+    each row, in `out` (log_probs_out) or in new tensors."""
+    import torch
+    classes = logits.shape[-1]
+    ptr, ld, rows = _rows(logits, "logits", logits.dtype, classes, logits.device)
+    n_given = 0 if given is None else int(given.shape[-1])
+    if out is None:
+        out = log_probs_out(rows, n_given, top, logits.device)
+    ptrs = []
+    for what, t, n, dtype in (("given", given, n_given, torch.int32), ("out.given", out.given, n_given, torch.float32),
+                              ("out.entropy", out.entropy, 1, torch.float32), ("out.top_ids", out.top_ids, top, torch.int32),
+                              ("out.top", out.top, top, torch.float32)):
+        if t is None or n == 0:
+            if n and what != "out.entropy":
+                raise ValueError(f"{what}: missing")
+            ptrs.append(None)
+            continue
+        if t.dtype != dtype or t.device != logits.device or not t.is_contiguous() or t.numel() != rows * n:
+            raise ValueError(f"{what}: need contiguous {dtype} of {rows} x {n} values on {logits.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        ptrs.append(t.data_ptr())
+    d = gi_log_probs_desc(rows, classes, ld, _gi_dtype(logits), temperature, n_given, top)
+    _check(_on(logits.device, stream, lambda s: lib().gi_log_probs(C.byref(d), ptr, *ptrs, s)), "gi_log_probs")
+    return out
 
 
 class Graph:

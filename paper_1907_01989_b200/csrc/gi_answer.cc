@@ -105,4 +105,41 @@ gi_status gi_linear_q4_run(const gi_linear_q4* layer, const void* dev_blob, cons
   return GI_OK;
 }
 
+gi_status gi_log_probs(const gi_log_probs_desc* d, const void* dev_logits, const int32_t* dev_given, float* dev_given_log_probs,
+                       float* dev_entropy, int32_t* dev_top_ids, float* dev_top_log_probs, void* stream) {
+  if (!d) return fail(GI_E_INVALID, "gi_log_probs: null descriptor");
+  if (d->rows < 0 || d->classes <= 0) return fail(GI_E_INVALID, "gi_log_probs: negative number of rows, or no classes");
+  if (d->rows > (1 << 28) || d->classes > (1 << 24)) return fail(GI_E_UNSUPPORTED, "gi_log_probs: more than 2^28 rows or 2^24 classes");
+  if (!known_dtype(d->dtype)) return fail(GI_E_INVALID, "gi_log_probs: dtype must be GI_F16, GI_BF16 or GI_F32");
+  if (!(d->temperature >= 1e-4f && d->temperature <= 1e4f)) return fail(GI_E_INVALID, "gi_log_probs: temperature must be 1e-4 .. 1e4");
+  if (d->n_given < 0 || d->n_given > 65536) return fail(GI_E_INVALID, "gi_log_probs: n_given must be 0 .. 65536");
+  if (d->top < 0 || d->top > GI_MAX_TOP || d->top > d->classes) return fail(GI_E_INVALID, "gi_log_probs: top must be 0 .. GI_MAX_TOP and at most classes");
+  if (d->rows == 0) return GI_OK;
+  if (!dev_logits || (d->n_given && (!dev_given || !dev_given_log_probs)) || (d->top && (!dev_top_ids || !dev_top_log_probs)))
+    return fail(GI_E_INVALID, "gi_log_probs: null argument");
+  if (!d->n_given && !d->top && !dev_entropy) return fail(GI_E_INVALID, "gi_log_probs: nothing asked for");
+  const int64_t ld = d->rows == 1 ? d->classes : d->ld;
+  if (ld < d->classes || ld > kMaxPitch) return fail(GI_E_INVALID, "gi_log_probs: ld below classes or too large");
+  if (!aligned_to(dev_logits, elem_of(d->dtype)) || !aligned_to(dev_given, 4) || !aligned_to(dev_given_log_probs, 4) || !aligned_to(dev_entropy, 4) ||
+      !aligned_to(dev_top_ids, 4) || !aligned_to(dev_top_log_probs, 4))
+    return fail(GI_E_INVALID, "gi_log_probs: a pointer not aligned to its elements");
+  LogProbsCall c;
+  c.x = dev_logits;
+  c.given = dev_given;
+  c.given_lp = dev_given_log_probs;
+  c.entropy = dev_entropy;
+  c.top_ids = dev_top_ids;
+  c.top_lp = dev_top_log_probs;
+  c.ld = ld;
+  c.rows = d->rows;
+  c.classes = d->classes;
+  c.n_given = d->n_given;
+  c.top = d->top;
+  c.dtype = d->dtype;
+  c.temperature = d->temperature;
+  const int err = launch_log_probs(c, stream);
+  if (err != 0) return fail(GI_E_CUDA, std::string("gi_log_probs: ") + cudaGetErrorString(static_cast<cudaError_t>(err)));
+  return GI_OK;
+}
+
 }  // extern "C"

@@ -159,4 +159,16 @@ LinearQ4Layout linear_q4_layout(int cin, int cout, int group, int scale_dtype, b
 void linear_q4_pack(const LinearQ4Weights& w, const float* bias, uint8_t* blob);  // blob: layout.bytes bytes
 int launch_linear_q4(const LinearQ4Call& c, void* stream);
 
+// Log probabilities of classes, entropy and leading classes of rows of logits (log_probs.cu).
+struct LogProbsCall {
+  const void* x = nullptr;
+  const int* given = nullptr;
+  float *given_lp = nullptr, *entropy = nullptr, *top_lp = nullptr;
+  int* top_ids = nullptr;
+  long long ld = 0;
+  int rows = 0, classes = 0, n_given = 0, top = 0, dtype = GI_F16;
+  float temperature = 1.0f;
+};
+int launch_log_probs(const LogProbsCall& c, void* stream);
+
 }  // namespace gi

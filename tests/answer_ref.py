@@ -45,3 +45,33 @@ def linear_q4(x, q, scales, zeros, bias, group, act="none"):
         y = y.clamp(min=0.0, max=6.0 if act == "relu6" else math.inf)
     sums = (x.shape[-1] * (3 if x.dtype == torch.float32 else 1) + 3) * 2.0 ** -23 * mag
     return y, sums + (y.abs() + sums) * UNIT[x.dtype] + TINY[x.dtype]
+
+
+def log_probs(logits, given=None, top=0, temperature=1.0):
+    """{"given", "entropy", "top", "top_ids"} in 64 bits, and {"log", "entropy"}: how far a kernel in fp32 may be off.
+
+    With d = (x - max) / T and p = softmax, an exponential is off by 4 |d| 2^-24 (its argument takes four roundings) and 2^-21 of
+    itself.  A thread adds up at most n = classes / 32 + 64 of them, each addition, and each change to a new maximum, off by 2^-22 at
+    most.  So ln S is off by n 2^-22 + 4 sum p |d| 2^-24; a log probability by that and four roundings of its own d, which is what
+    a caller adds as 2^-22 |log p|; and the entropy by the same errors of sum p d, each weighted with its d."""
+    x = logits.double().cpu() / float(np.float32(temperature))
+    rows, classes = x.shape
+    some = x.amax(1, keepdim=True) > -math.inf
+    d = torch.where(some, x - torch.where(some, x.amax(1, keepdim=True), 0.0), -math.inf)
+    log_s = torch.where(some, d.exp().sum(1, keepdim=True).log(), 0.0)
+    lp = d - log_s
+    p = lp.exp()
+    pd = torch.where(p > 0, p * d, 0.0)
+    out = {"entropy": torch.where(some[:, 0], log_s[:, 0] - pd.sum(1), 0.0)}
+    if given is not None:
+        g = given.cpu().long()
+        out["given"] = torch.where(g < 0, 0.0, torch.where(g < classes, lp.gather(1, g.clamp(0, classes - 1)), math.nan))
+    if top:
+        order = np.lexsort((np.broadcast_to(np.arange(classes), (rows, classes)), -logits.double().cpu().numpy()), axis=1)[:, :top]
+        out["top_ids"] = torch.from_numpy(np.ascontiguousarray(order)).int()
+        out["top"] = lp.gather(1, out["top_ids"].long())
+    n = (classes / 32 + 64) * 2.0 ** -22
+    absd = pd.abs().sum(1)
+    ln = n + 4 * absd * 2.0 ** -24
+    ent = (1 + absd) * ln + 4 * torch.where(p > 0, p * d * d, 0.0).sum(1) * 2.0 ** -24 + n * absd
+    return out, {"log": ln, "entropy": ent}
