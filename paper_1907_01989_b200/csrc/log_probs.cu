@@ -48,42 +48,6 @@ struct Params {
   int ks;          // CTAs of a row
 };
 
-template <int XT>
-struct Elem;
-template <>
-struct Elem<GI_F16> {
-  typedef __half type;
-  static constexpr int kVec = 8;
-  static __device__ __forceinline__ float f32(__half v) { return __half2float(v); }
-};
-template <>
-struct Elem<GI_BF16> {
-  typedef __nv_bfloat16 type;
-  static constexpr int kVec = 8;
-  static __device__ __forceinline__ float f32(__nv_bfloat16 v) { return __bfloat162float(v); }
-};
-template <>
-struct Elem<GI_F32> {
-  typedef float type;
-  static constexpr int kVec = 4;
-  static __device__ __forceinline__ float f32(float v) { return v; }
-};
-
-// ordered bits of a value above the inverted class: larger values first, then lower classes; a NaN above all, -0 as 0
-__device__ __forceinline__ u64 key_of(float v, int i) {
-  int b = __float_as_int(v + 0.0f);
-  if (v != v) b = 0x7fffffff;
-  const unsigned o = static_cast<unsigned>(b ^ ((b >> 31) & 0x7fffffff)) ^ 0x80000000u;
-  return (static_cast<u64>(o) << 32) | (0xffffffffu - static_cast<unsigned>(i));
-}
-__device__ __forceinline__ int class_of(u64 k) { return static_cast<int>(0xffffffffu - static_cast<unsigned>(k)); }
-__device__ __forceinline__ float value_of(u64 k) {
-  const int o = static_cast<int>(static_cast<unsigned>(k >> 32) ^ 0x80000000u);
-  return __int_as_float(o ^ ((o >> 31) & 0x7fffffff));
-}
-__device__ __forceinline__ u64 max64(u64 a, u64 b) { return a > b ? a : b; }
-__device__ __forceinline__ u64 shfl_xor64(u64 v, int m) { return __shfl_xor_sync(0xffffffffu, v, m); }
-
 __device__ __forceinline__ float ex2(float v) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
@@ -93,6 +57,84 @@ __device__ __forceinline__ float ex2(float v) {
 __device__ __forceinline__ float max_nan(float a, float b) {
   float r;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+template <int XT>
+struct Elem;
+template <>
+struct Elem<GI_F16> {
+  typedef __half type;
+  static constexpr int kVec = 8;
+  static __device__ __forceinline__ __half none() { return __ushort_as_half(0xfc00); }
+  static __device__ __forceinline__ float f32(__half v) { return __half2float(v); }
+  static __device__ __forceinline__ float most(const uint4& w) {  // the largest of 16 bytes, a NaN if there is one
+    const __half2* h = reinterpret_cast<const __half2*>(&w);
+    const float2 m = __half22float2(__hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3])));
+    return max_nan(m.x, m.y);
+  }
+};
+template <>
+struct Elem<GI_BF16> {
+  typedef __nv_bfloat16 type;
+  static constexpr int kVec = 8;
+  static __device__ __forceinline__ __nv_bfloat16 none() { return __ushort_as_bfloat16(0xff80); }
+  static __device__ __forceinline__ float f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+  static __device__ __forceinline__ float most(const uint4& w) {
+    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&w);
+    const float2 m = __bfloat1622float2(__hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3])));
+    return max_nan(m.x, m.y);
+  }
+};
+template <>
+struct Elem<GI_F32> {
+  typedef float type;
+  static constexpr int kVec = 4;
+  static __device__ __forceinline__ float none() { return -INFINITY; }
+  static __device__ __forceinline__ float f32(float v) { return v; }
+  static __device__ __forceinline__ float most(const uint4& w) {
+    return max_nan(max_nan(__uint_as_float(w.x), __uint_as_float(w.y)), max_nan(__uint_as_float(w.z), __uint_as_float(w.w)));
+  }
+};
+
+// a value's bits as a whole number of the same order; a NaN above all, -0 as 0
+__device__ __forceinline__ int ordered(float v) {
+  int b = __float_as_int(v + 0.0f);
+  if (v != v) b = 0x7fffffff;
+  return b ^ ((b >> 31) & 0x7fffffff);
+}
+// that above the inverted class: larger values first, then lower classes
+__device__ __forceinline__ u64 key_of(float v, int i) {
+  return (static_cast<u64>(static_cast<unsigned>(ordered(v)) ^ 0x80000000u) << 32) | (0xffffffffu - static_cast<unsigned>(i));
+}
+__device__ __forceinline__ int class_of(u64 k) { return static_cast<int>(0xffffffffu - static_cast<unsigned>(k)); }
+__device__ __forceinline__ float value_of(u64 k) {
+  const int o = static_cast<int>(static_cast<unsigned>(k >> 32) ^ 0x80000000u);
+  return __int_as_float(o ^ ((o >> 31) & 0x7fffffff));
+}
+__device__ __forceinline__ u64 max64(u64 a, u64 b) { return a > b ? a : b; }
+__device__ __forceinline__ u64 shfl_xor64(u64 v, int m) { return __shfl_xor_sync(0xffffffffu, v, m); }
+
+// two fp32 numbers in a register pair: one instruction for both
+__device__ __forceinline__ u64 pack2(float a, float b) {
+  u64 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpack2(u64 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ u64 add2(u64 a, u64 b) {
+  u64 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ u64 mul2(u64 a, u64 b) {
+  u64 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ u64 fma2(u64 a, u64 b, u64 c) {
+  u64 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
   return r;
 }
 
@@ -116,27 +158,16 @@ struct Stat {
     s += e;
     t = fmaf(e, d, t);
   }
-  __device__ __forceinline__ void merge(Stat o, float c) {
-    const float to = fmaxf(m, o.m);
-    rebase(to, c);
-    o.rebase(to, c);
-    s += o.s;
-    t += o.t;
-  }
 };
 
+// the sums of the lanes of every group of `width`: one change of maximum, then sums that come out the same in every lane
 __device__ __forceinline__ Stat warp_merge(Stat st, float c, int width) {
+  float m = st.m;
+  for (int o = 1; o < width; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  st.rebase(m, c);
   for (int o = 1; o < width; o <<= 1) {
-    Stat other;
-    other.m = __shfl_xor_sync(0xffffffffu, st.m, o);
-    other.s = __shfl_xor_sync(0xffffffffu, st.s, o);
-    other.t = __shfl_xor_sync(0xffffffffu, st.t, o);
-    // both lanes of a pair add the same two in the same order
-    const bool low = (threadIdx.x & o) == 0;
-    Stat a = low ? st : other;
-    const Stat b = low ? other : st;
-    a.merge(b, c);
-    st = a;
+    st.s += __shfl_xor_sync(0xffffffffu, st.s, o);
+    st.t += __shfl_xor_sync(0xffffffffu, st.t, o);
   }
   return st;
 }
@@ -169,45 +200,114 @@ struct Row {
     for (int j = 0; j < V; ++j) v[j] = Elem<XT>::f32(e[j]);
   }
   __device__ __forceinline__ float at(int c) const { return Elem<XT>::f32(x[c]); }
+  // piece i; beside the row, and where there is no such piece, minus infinity: that adds nothing to a sum
+  __device__ __forceinline__ uint4 piece(int i) const {
+    if (whole(i)) return raw(i);
+    uint4 w;
+    T* e = reinterpret_cast<T*>(&w);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const int cl = i * V - lead + j;
+      e[j] = cl >= 0 && cl < classes ? x[cl] : Elem<XT>::none();
+    }
+    return w;
+  }
 };
 
-// What a thread has seen of a row: sums, and its largest element.
+// What a thread has seen of a row: sums, two at a time, and its largest element - as the first of the 16-byte pieces that hold a
+// largest one (looking for the element at every new maximum, which some lane of a warp meets at almost every piece, took two thirds
+// of the instructions).
 template <int XT>
 struct Seen {
   static constexpr int V = Elem<XT>::kVec;
-  Stat st;
-  u64 best;
-  float best_v;  // NaN: every element is looked at
+  float m;
+  u64 s, t;
+  int most;    // ordered bits of the largest element of whole pieces; below all of them at first
+  uint4 where; // it
+  int at;      // class of its first element
   __device__ __forceinline__ void clear() {
-    st.clear();
-    best = 0;
-    best_v = __int_as_float(0x7fffffff);
+    m = kLowest;
+    s = t = 0;
+    most = static_cast<int>(0x80000000u);
+    where = make_uint4(0u, 0u, 0u, 0u);
+    at = 0;
   }
-  __device__ __forceinline__ void piece(const float (&v)[V], int c0, float c) {
-    float pm = v[0];
+  __device__ __forceinline__ void grow(float to, float c) {
+    if (!(to > m)) return;
+    const float e = fmaxf((m - to) * c, -1.0e30f), f = ex2(e);
+    t = mul2(fma2(pack2(e, e), s, t), pack2(f, f));
+    s = mul2(s, pack2(f, f));
+    m = to;
+  }
+  // N pieces, their first elements' classes `step` apart
+  template <int N>
+  __device__ __forceinline__ void pieces(const uint4 (&w)[N], int c0, int step, float c) {
+    float pm[N], top;
 #pragma unroll
-    for (int j = 1; j < V; ++j) pm = max_nan(pm, v[j]);
-    if (!(pm <= best_v)) {
+    for (int j = 0; j < N; ++j) pm[j] = Elem<XT>::most(w[j]);
 #pragma unroll
-      for (int j = 0; j < V; ++j) best = max64(best, key_of(v[j], c0 + j));
-      best_v = value_of(best);
+    for (int j = 0; j < N; ++j) {
+      const int o = ordered(pm[j]);
+      if (o > most) {
+        most = o;
+        where = w[j];
+        at = c0 + j * step;
+      }
     }
-    if (pm > st.m) st.rebase(pm, c);
+    top = pm[0];
 #pragma unroll
-    for (int j = 0; j < V; ++j) st.add(v[j], c);
-  }
-  __device__ __forceinline__ void one(float v, int cl, float c) {
-    best = max64(best, key_of(v, cl));
-    best_v = value_of(best);
-    if (v > st.m) st.rebase(v, c);
-    st.add(v, c);
-  }
-  // piece i of a row, if there is one
-  __device__ __forceinline__ void edge(const Row<XT>& row, int i, float c) {
-    for (int j = 0; j < V; ++j) {
-      const int cl = i * V - row.lead + j;
-      if (cl >= 0 && cl < row.classes) one(row.at(cl), cl, c);
+    for (int j = 1; j < N; ++j) top = max_nan(top, pm[j]);
+    grow(top, c);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      float v[V];
+      Row<XT>::convert(w[j], v);
+      add(v, c);
     }
+  }
+  __device__ __forceinline__ void add(const float (&v)[V], float c) {
+    const u64 minus = pack2(-m, -m), c2 = pack2(c, c);
+#pragma unroll
+    for (int k = 0; k < V; k += 2) {
+      float d0, d1;
+      unpack2(mul2(add2(pack2(v[k], v[k + 1]), minus), c2), d0, d1);
+      d0 = max_nan(d0, -1000.0f);  // (see Stat)
+      d1 = max_nan(d1, -1000.0f);
+      const u64 e = pack2(ex2(d0), ex2(d1));
+      s = add2(s, e);
+      t = fma2(e, pack2(d0, d1), t);
+    }
+  }
+  // the pieces first, first + stride, ... of a row, N requested at a time
+  template <int N>
+  __device__ __forceinline__ void walk(const Row<XT>& row, int first, int stride, float c) {
+    for (int i = first; i < row.pieces; i += N * stride) {
+      uint4 w[N];
+#pragma unroll
+      for (int j = 0; j < N; ++j) w[j] = row.piece(i + j * stride);
+      pieces(w, i * V - row.lead, stride * V, c);
+    }
+  }
+  __device__ __forceinline__ Stat stat() const {
+    Stat st;
+    float a, b;
+    st.m = m;
+    unpack2(s, a, b);
+    st.s = a + b;
+    unpack2(t, a, b);
+    st.t = a + b;
+    return st;
+  }
+  __device__ __forceinline__ u64 best(const Row<XT>& row) const {
+    u64 k = 0;
+    if (most != static_cast<int>(0x80000000u)) {
+      float v[V];
+      Row<XT>::convert(where, v);
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (at + j >= 0 && at + j < row.classes) k = max64(k, key_of(v[j], at + j));
+    }
+    return k;
   }
 };
 
@@ -226,7 +326,7 @@ constexpr int kGroups = 64;    // groups of 4 threads, whose largest elements bo
 constexpr int kFound = 1024;   // elements collected at a time
 
 struct Shared {
-  u64 group[kGroups];
+  alignas(16) u64 group[kGroups];
   u64 found[kFound];
   u64 best[kMaxTop];     // this CTA's answer, largest first; 0: none
   Stat warp[kWarps], st;
@@ -241,47 +341,30 @@ __global__ void __launch_bounds__(kThreads) row_kernel(const Params p) {
   extern __shared__ __align__(16) unsigned char raw_smem[];
   Shared& sh = *reinterpret_cast<Shared*>(raw_smem);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const long long r = blockIdx.x / p.ks;
   const int rank = blockIdx.x % p.ks;
+  const long long r = blockIdx.x / p.ks;
+  const int stride = kThreads * p.ks, first = rank * kThreads + tid;
   pdl_launch_dependents();
   pdl_wait();
   const Row<XT> row(p, r);
-  const int stride = kThreads * p.ks, first = rank * kThreads + tid;
+  // the classes asked for, and their logits: two requests one after the other, answered while the row is read
+  int id0 = -1;
+  float given0 = 0.0f;
+  if (rank == 0 && tid < p.n_given) {
+    id0 = p.given[r * p.n_given + tid];
+    if (id0 >= 0 && id0 < p.classes) given0 = row.at(id0);
+  }
   // pieces of this thread: first, first + stride, ...; the row's first and last may be cut
   Seen<XT> seen;
   seen.clear();
-  int i = first;
-  if (i < row.pieces && !row.whole(i)) {
-    seen.edge(row, i, p.c);
-    i += stride;
-  }
-  for (; i + 3 * stride < row.pieces && row.whole(i + 3 * stride); i += 4 * stride) {
-    uint4 w[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = row.raw(i + j * stride);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float v[V];
-      Row<XT>::convert(w[j], v);
-      seen.piece(v, (i + j * stride) * V - row.lead, p.c);
-    }
-  }
-  for (; i < row.pieces; i += stride) {
-    if (row.whole(i)) {
-      float v[V];
-      Row<XT>::convert(row.raw(i), v);
-      seen.piece(v, i * V - row.lead, p.c);
-    } else {
-      seen.edge(row, i, p.c);
-    }
-  }
-
+  seen.template walk<4>(row, first, stride, p.c);
   {
-    const Stat st = warp_merge(seen.st, p.c, 32);
+    const Stat st = warp_merge(seen.stat(), p.c, 32);
     if (lane == 0) sh.warp[warp] = st;
   }
   if (p.top) {
-    u64 g = max64(seen.best, shfl_xor64(seen.best, 1));
+    u64 g = seen.best(row);
+    g = max64(g, shfl_xor64(g, 1));
     g = max64(g, shfl_xor64(g, 2));
     if ((tid & 3) == 0) sh.group[tid >> 2] = g;
     if (tid == 0) {
@@ -291,17 +374,20 @@ __global__ void __launch_bounds__(kThreads) row_kernel(const Params p) {
     if (tid < kMaxTop) sh.best[tid] = 0;
   }
   __syncthreads();
-  if (tid == 0) {
-    Stat st = sh.warp[0];
-    for (int k = 1; k < kWarps; ++k) st.merge(sh.warp[k], p.c);
-    sh.st = st;
+  if (warp == kWarps - 1) {
+    const Stat st = warp_merge(sh.warp[lane % kWarps], p.c, kWarps);
+    if (lane == 0) sh.st = st;
   }
   if (p.top) {
     // the `top` groups whose largest elements lead (all with elements, where these are fewer), and the least of those
     if (tid < kGroups) {
       const u64 mine = sh.group[tid];
       int above = 0;
-      for (int k = 0; k < kGroups; ++k) above += sh.group[k] > mine;
+#pragma unroll 8
+      for (int k = 0; k < kGroups; k += 2) {
+        const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(&sh.group[k]);
+        above += (two.x > mine) + (two.y > mine);
+      }
       if (mine && above < p.top) sh.win[atomicAdd(&sh.n_win, 1)] = tid;
       if (mine && above == p.top - 1) sh.bound = mine;
     }
@@ -315,26 +401,15 @@ __global__ void __launch_bounds__(kThreads) row_kernel(const Params p) {
         // this group's pieces again: lane l takes those of thread l % 4
         for (int q = rank * kThreads + sh.win[k] * 4 + (lane & 3) + (lane >> 2) * stride; q < row.pieces; q += 8 * stride) {
           const int c0 = q * V - row.lead;
-          if (row.whole(q)) {
-            float v[V];
-            Row<XT>::convert(row.raw(q), v);
+          float v[V];
+          Row<XT>::convert(row.piece(q), v);
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-              if (bound && v[j] < bound_v) continue;
-              const u64 key = key_of(v[j], c0 + j);
-              if (key >= bound) {
-                const int at = atomicAdd(&sh.n_found, 1);
-                if (at < kFound) sh.found[at] = key;
-              }
-            }
-          } else {
-            for (int j = 0; j < V; ++j) {
-              if (c0 + j < 0 || c0 + j >= row.classes) continue;
-              const u64 key = key_of(row.at(c0 + j), c0 + j);
-              if (key >= bound) {
-                const int at = atomicAdd(&sh.n_found, 1);
-                if (at < kFound) sh.found[at] = key;
-              }
+          for (int j = 0; j < V; ++j) {
+            if ((bound && v[j] < bound_v) || c0 + j < 0 || c0 + j >= row.classes) continue;
+            const u64 key = key_of(v[j], c0 + j);
+            if (key >= bound) {
+              const int at = atomicAdd(&sh.n_found, 1);
+              if (at < kFound) sh.found[at] = key;
             }
           }
         }
@@ -360,17 +435,15 @@ __global__ void __launch_bounds__(kThreads) row_kernel(const Params p) {
     if (rank == 0) {
       // the other CTAs' sums and answers, in the order of the CTAs
       const unsigned at = smem_u32(&sh);
-      if (tid == 0) {
-        Stat st = sh.st;
-        for (int k = 1; k < p.ks; ++k) {
-          const unsigned from = mapa_shared(at + static_cast<unsigned>(reinterpret_cast<unsigned char*>(&sh.st) - raw_smem), k);
-          Stat o;
-          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o.m) : "r"(from) : "memory");
-          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o.s) : "r"(from + 4) : "memory");
-          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o.t) : "r"(from + 8) : "memory");
-          st.merge(o, p.c);
-        }
-        sh.st = st;
+      if (warp == kWarps - 1) {
+        const unsigned from = mapa_shared(at + static_cast<unsigned>(reinterpret_cast<unsigned char*>(&sh.st) - raw_smem), lane % p.ks);
+        Stat st;
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(st.m) : "r"(from) : "memory");
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(st.s) : "r"(from + 4) : "memory");
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(st.t) : "r"(from + 8) : "memory");
+        st = warp_merge(st, p.c, p.ks);
+        __syncwarp();
+        if (lane == 0) sh.st = st;  // (nobody else reads this CTA's)
       }
       const int n = p.ks * p.top;
       for (int k = tid; k < n; k += kThreads) {
@@ -396,7 +469,8 @@ __global__ void __launch_bounds__(kThreads) row_kernel(const Params p) {
     const float log_s = logf(st.s);
     if (tid == 0 && p.entropy) p.entropy[r] = entropy_of(st, log_s);
     if (tid < p.top) write_top(p, r, tid, sh.best[tid], st, log_s);
-    for (int j = tid; j < p.n_given; j += kThreads) {
+    if (tid < p.n_given) write_given(p, r, tid, st, log_s, given0, id0);
+    for (int j = tid + kThreads; j < p.n_given; j += kThreads) {
       const int id = p.given[r * p.n_given + j];
       write_given(p, r, j, st, log_s, id >= 0 && id < p.classes ? row.at(id) : 0.0f, id);
     }
@@ -407,7 +481,8 @@ __global__ void __launch_bounds__(kThreads) row_kernel(const Params p) {
 // ---------------------------------------------------------------- a warp for a row
 constexpr int kWarpFound = 128;
 
-template <int XT>
+// N: pieces that a lane requests at a time.
+template <int XT, int N>
 __global__ void __launch_bounds__(kThreads) warp_kernel(const Params p) {
   constexpr int V = Elem<XT>::kVec;
   __shared__ u64 found_all[kWarps][kWarpFound];
@@ -418,81 +493,58 @@ __global__ void __launch_bounds__(kThreads) warp_kernel(const Params p) {
   if (r >= p.rows) return;
   u64* found = found_all[warp];
   const Row<XT> row(p, r);
+  int id0 = -1;
+  float given0 = 0.0f;
+  if (lane < p.n_given) {
+    id0 = p.given[r * p.n_given + lane];
+    if (id0 >= 0 && id0 < p.classes) given0 = row.at(id0);
+  }
   Seen<XT> seen;
   seen.clear();
-  for (int i = lane; i < row.pieces; i += 32) {
-    if (row.whole(i)) {
-      float v[V];
-      Row<XT>::convert(row.raw(i), v);
-      seen.piece(v, i * V - row.lead, p.c);
-    } else {
-      seen.edge(row, i, p.c);
-    }
-  }
-  const Stat st = warp_merge(seen.st, p.c, 32);
+  seen.template walk<N>(row, lane, 32, p.c);
+  const Stat st = warp_merge(seen.stat(), p.c, 32);
   const float log_s = logf(st.s);
   if (lane == 0 && p.entropy) p.entropy[r] = entropy_of(st, log_s);
-  for (int j = lane; j < p.n_given; j += 32) {
+  if (lane < p.n_given) write_given(p, r, lane, st, log_s, given0, id0);
+  for (int j = lane + 32; j < p.n_given; j += 32) {
     const int id = p.given[r * p.n_given + j];
     write_given(p, r, j, st, log_s, id >= 0 && id < p.classes ? row.at(id) : 0.0f, id);
   }
   if (p.top == 0) return;
-  u64 mine = seen.best;
   if (p.top == 1) {
+    u64 mine = seen.best(row);
 #pragma unroll
     for (int o = 16; o; o >>= 1) mine = max64(mine, shfl_xor64(mine, o));
     if (lane == 0) write_top(p, r, 0, mine, st, log_s);
     return;
   }
-  // the least of the `top` leading lanes' largest elements bounds the answer
+  // The least of the `top` leading lanes' largest values bounds the answer from below (equal values count together); a lane without
+  // elements has the least of all, which every element reaches.
   int above = 0;
 #pragma unroll
-  for (int k = 0; k < 32; ++k) above += __shfl_sync(0xffffffffu, mine, k) > mine;
-  const unsigned edge = __ballot_sync(0xffffffffu, mine != 0 && above == p.top - 1);
-  const u64 bound = edge ? __shfl_sync(0xffffffffu, mine, __ffs(edge) - 1) : 0;
-  // every lane's elements that reach it, lane by lane; as many as fit
+  for (int k = 0; k < 32; ++k) above += __shfl_sync(0xffffffffu, seen.most, k) > seen.most;
+  const int bound = __reduce_min_sync(0xffffffffu, above < p.top ? seen.most : 0x7fffffff);
+  // every lane's elements that reach it; as many as fit
   int n = 0;
-  const bool look = mine != 0 && mine >= bound;
-  const float bound_v = value_of(bound);
+  const unsigned before = (1u << lane) - 1u;
   for (int i = lane; __any_sync(0xffffffffu, i < row.pieces); i += 32) {
-    const int c0 = i * V - row.lead;
-    unsigned hits = 0;
     float v[V];
-    if (look && i < row.pieces) {
-      if (row.whole(i)) {
-        Row<XT>::convert(row.raw(i), v);
+    const int c0 = i * V - row.lead;
+    const bool look = i < row.pieces && seen.most >= bound;
+    if (look) Row<XT>::convert(row.piece(i), v);
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-          if (!(bound && v[j] < bound_v) && key_of(v[j], c0 + j) >= bound) hits |= 1u << j;
-      } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-          if (c0 + j >= 0 && c0 + j < row.classes) {
-            v[j] = row.at(c0 + j);
-            if (key_of(v[j], c0 + j) >= bound) hits |= 1u << j;
-          }
-      }
+    for (int j = 0; j < V; ++j) {
+      const bool hit = look && ordered(v[j]) >= bound && c0 + j >= 0 && c0 + j < row.classes;
+      const unsigned hits = __ballot_sync(0xffffffffu, hit);
+      if (!hits) continue;
+      const int at = n + __popc(hits & before);
+      if (hit && at < kWarpFound) found[at] = key_of(v[j], c0 + j);
+      n += __popc(hits);
     }
-    if (!__any_sync(0xffffffffu, hits != 0)) continue;
-    // places for this round's, in the order of the lanes
-    const int count = __popc(hits);
-    int upto = count;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int u = __shfl_up_sync(0xffffffffu, upto, o);
-      if (lane >= o) upto += u;
-    }
-    int at = n + upto - count;
-#pragma unroll
-    for (int j = 0; j < V; ++j)
-      if (hits >> j & 1u) {
-        if (at < kWarpFound) found[at] = key_of(v[j], c0 + j);
-        ++at;
-      }
-    n += __shfl_sync(0xffffffffu, upto, 31);
   }
   __syncwarp();
   if (n <= kWarpFound) {
+    // an element's place is the number of larger ones
     for (int k = lane; k < n; k += 32) {
       const u64 key = found[k];
       int place = 0;
@@ -501,17 +553,20 @@ __global__ void __launch_bounds__(kThreads) warp_kernel(const Params p) {
     }
     return;
   }
-  // more than fit: one after the other, each lane's largest element below the last one
+  // more than fit (many equal ones): one after the other, each lane's largest element below the last one
   u64 last = ~0ull;
   for (int k = 0; k < p.top; ++k) {
     u64 best = 0;
-    for (int i = lane; i < row.pieces; i += 32)
+    for (int i = lane; i < row.pieces; i += 32) {
+      float v[V];
+      Row<XT>::convert(row.piece(i), v);
+#pragma unroll
       for (int j = 0; j < V; ++j) {
         const int cl = i * V - row.lead + j;
-        if (cl < 0 || cl >= row.classes) continue;
-        const u64 key = key_of(row.at(cl), cl);
-        if (key < last) best = max64(best, key);
+        const u64 key = key_of(v[j], cl);
+        if (cl >= 0 && cl < row.classes && key < last) best = max64(best, key);
       }
+    }
 #pragma unroll
     for (int o = 16; o; o >>= 1) best = max64(best, shfl_xor64(best, o));
     if (lane == 0) write_top(p, r, k, best, st, log_s);
@@ -523,73 +578,138 @@ __global__ void __launch_bounds__(kThreads) warp_kernel(const Params p) {
 constexpr int kFew = 64;         // classes
 constexpr int kThreadRows = 128; // rows of a CTA
 
-template <int XT>
+// LEAST, MOST: the fewest and the most classes.
+template <int XT, int LEAST, int MOST>
 __global__ void __launch_bounds__(kThreadRows) thread_kernel(const Params p) {
   typedef typename Elem<XT>::type T;
   constexpr int V = Elem<XT>::kVec;
   extern __shared__ __align__(16) unsigned char raw_smem[];
-  T* xs = reinterpret_cast<T*>(raw_smem);
-  pdl_launch_dependents();
-  pdl_wait();
-  const long long r0 = static_cast<long long>(blockIdx.x) * kThreadRows;
-  const int n = static_cast<int>(min(static_cast<long long>(kThreadRows), p.rows - r0));
-  const T* x = static_cast<const T*>(p.x) + r0 * p.ld;
-  int lead = 0;
-  if (p.ld == p.classes) {
-    // the rows are one run of memory: whole pieces of it, and what lies at its ends by elements
-    lead = static_cast<int>(reinterpret_cast<unsigned long long>(x) / sizeof(T) % V);
-    const int total = n * p.classes, pieces = (lead + total + V - 1) / V;
-    for (int i = threadIdx.x; i < pieces; i += kThreadRows) {
-      const int e = i * V - lead;
-      if (e >= 0 && e + V <= total) {
-        *reinterpret_cast<uint4*>(xs + i * V) = __ldg(reinterpret_cast<const uint4*>(x + e));
-      } else {
-        for (int j = 0; j < V; ++j)
-          if (e + j >= 0 && e + j < total) xs[i * V + j] = x[e + j];
+  const int buffer = kThreadRows * p.classes + 2 * V;  // elements
+  const long long tiles = (static_cast<long long>(p.rows) + kThreadRows - 1) / kThreadRows;
+  // the rows of a tile into one of two buffers; the elements in front of the first one's, where they are copied by whole pieces
+  auto fetch = [&](long long tile, int which) {
+    T* xs = reinterpret_cast<T*>(raw_smem) + which * buffer;
+    const long long r0 = tile * kThreadRows;
+    const int n = static_cast<int>(min(static_cast<long long>(kThreadRows), p.rows - r0));
+    const T* x = static_cast<const T*>(p.x) + r0 * p.ld;
+    int lead = 0;
+    if (p.ld == p.classes) {
+      // the rows are one run of memory: whole pieces of it, and what lies at its ends by elements
+      lead = static_cast<int>(reinterpret_cast<unsigned long long>(x) / sizeof(T) % V);
+      const int total = n * p.classes, pieces = (lead + total + V - 1) / V;
+      for (int i = threadIdx.x; i < pieces; i += kThreadRows) {
+        const int e = i * V - lead;
+        if (e >= 0 && e + V <= total) {
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(xs + i * V)), "l"(x + e) : "memory");
+        } else {
+          for (int j = 0; j < V; ++j)
+            if (e + j >= 0 && e + j < total) xs[i * V + j] = x[e + j];
+        }
+      }
+    } else {
+      for (int k = threadIdx.x; k < n * p.classes; k += kThreadRows) {
+        const int row = k / p.classes;
+        xs[k] = x[row * p.ld + (k - row * p.classes)];
       }
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    return lead;
+  };
+  pdl_launch_dependents();
+  pdl_wait();
+  int lead = fetch(blockIdx.x, 0);
+  int id = -1;  // the first class asked for
+  if (p.n_given && static_cast<long long>(blockIdx.x) * kThreadRows + threadIdx.x < p.rows)
+    id = p.given[(static_cast<long long>(blockIdx.x) * kThreadRows + threadIdx.x) * p.n_given];
+  for (long long tile = blockIdx.x, which = 0; tile < tiles; tile += gridDim.x, which ^= 1) {
+  const long long next = tile + gridDim.x, r = tile * kThreadRows + threadIdx.x;
+  int next_lead = 0, next_id = -1;
+  __syncthreads();  // the other buffer has been read
+  if (next < tiles) {
+    next_lead = fetch(next, static_cast<int>(which ^ 1));
+    if (p.n_given && next * kThreadRows + threadIdx.x < p.rows) next_id = p.given[(next * kThreadRows + threadIdx.x) * p.n_given];
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
   } else {
-    for (int k = threadIdx.x; k < n * p.classes; k += kThreadRows) {
-      const int row = k / p.classes;
-      xs[k] = x[row * p.ld + (k - row * p.classes)];
-    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
   }
   __syncthreads();
-  if (static_cast<int>(threadIdx.x) >= n) return;
-  const T* mine = xs + lead + threadIdx.x * p.classes;
-  const long long r = r0 + threadIdx.x;
+  if (r < p.rows) {
+  const T* mine = reinterpret_cast<const T*>(raw_smem) + which * buffer + lead + threadIdx.x * p.classes;
+  // the row in registers; behind its last class minus infinity, which adds nothing and, as a later class, leads nothing
+  float v[MOST];
+#pragma unroll
+  for (int j = 0; j < MOST; ++j) v[j] = j < LEAST || j < p.classes ? Elem<XT>::f32(mine[j]) : -INFINITY;
+  float high = v[0];
+#pragma unroll
+  for (int j = 1; j < MOST; ++j) high = max_nan(high, v[j]);
   Stat st;
-  st.clear();
-  float high = Elem<XT>::f32(mine[0]);
-  int where = 0;
-  bool nan = high != high;
-  for (int j = 1; j < p.classes; ++j) {
-    const float v = Elem<XT>::f32(mine[j]);
-    if (v > high || (v != v && !nan)) {  // the first NaN leads, as in key_of
-      high = v;
-      where = j;
-      nan = v != v;
-    }
-  }
   st.m = high > kLowest ? high : kLowest;  // (also where it is a NaN: the sums become one)
-  for (int j = 0; j < p.classes; ++j) st.add(Elem<XT>::f32(mine[j]), p.c);
+  u64 s = 0, t = 0;
+  const u64 minus = pack2(-st.m, -st.m), c2 = pack2(p.c, p.c);
+#pragma unroll
+  for (int j = 0; j < MOST; j += 2) {
+    float d0, d1;
+    unpack2(mul2(add2(pack2(v[j], v[j + 1]), minus), c2), d0, d1);
+    d0 = max_nan(d0, -1000.0f);  // (see Stat)
+    d1 = max_nan(d1, -1000.0f);
+    const u64 e = pack2(ex2(d0), ex2(d1));
+    s = add2(s, e);
+    t = fma2(e, pack2(d0, d1), t);
+  }
+  float a, b;
+  unpack2(s, a, b);
+  st.s = a + b;
+  unpack2(t, a, b);
+  st.t = a + b;
   const float log_s = logf(st.s);
   if (p.entropy) p.entropy[r] = entropy_of(st, log_s);
   for (int j = 0; j < p.n_given; ++j) {
-    const int id = p.given[r * p.n_given + j];
+    if (j) id = p.given[r * p.n_given + j];
     write_given(p, r, j, st, log_s, id >= 0 && id < p.classes ? Elem<XT>::f32(mine[id]) : 0.0f, id);
   }
-  if (p.top == 0) return;
-  u64 last = key_of(high, where);
-  write_top(p, r, 0, last, st, log_s);
-  for (int k = 1; k < p.top; ++k) {
-    u64 best = 0;
-    for (int j = 0; j < p.classes; ++j) {
-      const u64 key = key_of(Elem<XT>::f32(mine[j]), j);
-      if (key < last) best = max64(best, key);
+  if (p.top) {
+  int where = 0;  // the first of the largest
+#pragma unroll
+  for (int j = MOST - 1; j >= 0; --j) where = v[j] == high ? j : where;
+  if (high != high) {  // or the first NaN
+#pragma unroll
+    for (int j = MOST - 1; j >= 0; --j) where = v[j] != v[j] ? j : where;
+  }
+  p.top_ids[r * p.top] = where;
+  p.top_lp[r * p.top] = log_prob(high, st, log_s, p.inv_t);
+  if (p.top > 1) {
+  if (XT != GI_F32) {
+    // the ordered bits of a value of 16 bits leave at least 13 low ones to themselves: the class goes there
+    int key[MOST];
+#pragma unroll
+    for (int j = 0; j < MOST; ++j) key[j] = j < p.classes ? (ordered(v[j]) & ~(kFew - 1)) | (kFew - 1 - j) : static_cast<int>(0x80000000u);
+    int last = 0x7fffffff;
+    for (int k = 0; k < p.top; ++k) {
+      int best = static_cast<int>(0x80000000u);
+#pragma unroll
+      for (int j = 0; j < MOST; ++j) best = max(best, key[j] < last ? key[j] : static_cast<int>(0x80000000u));
+      const int id = kFew - 1 - (best & (kFew - 1));
+      p.top_ids[r * p.top + k] = id;
+      p.top_lp[r * p.top + k] = log_prob(Elem<XT>::f32(mine[id]), st, log_s, p.inv_t);
+      last = best;
     }
-    write_top(p, r, k, best, st, log_s);
-    last = best;
+  } else {
+    u64 last = key_of(high, where);
+    for (int k = 1; k < p.top; ++k) {
+      u64 best = 0;
+      for (int j = 0; j < p.classes; ++j) {
+        const u64 key = key_of(Elem<XT>::f32(mine[j]), j);
+        if (key < last) best = max64(best, key);
+      }
+      write_top(p, r, k, best, st, log_s);
+      last = best;
+    }
+  }
+  }
+  }
+  }
+  lead = next_lead;
+  id = next_id;
   }
 }
 
@@ -598,15 +718,26 @@ cudaError_t launch_type(Params& p, cudaStream_t stream) {
   constexpr int V = Elem<XT>::kVec;
   const int sms = device_sm_count();
   if (p.classes <= kFew && p.rows >= 4096) {
-    const unsigned grid = static_cast<unsigned>((static_cast<long long>(p.rows) + kThreadRows - 1) / kThreadRows);
-    return launch_pdl(thread_kernel<XT>, dim3(grid), dim3(kThreadRows), (kThreadRows * p.classes + 2 * V) * sizeof(typename Elem<XT>::type), stream, p);
+    const unsigned grid = static_cast<unsigned>(std::min<long long>((static_cast<long long>(p.rows) + kThreadRows - 1) / kThreadRows, 8 * sms));
+    const size_t smem = 2 * (kThreadRows * p.classes + 2 * V) * sizeof(typename Elem<XT>::type);
+    void (*k)(const Params) = p.classes <= 8    ? thread_kernel<XT, 1, 8>
+                              : p.classes <= 16 ? thread_kernel<XT, 9, 16>
+                              : p.classes <= 24 ? thread_kernel<XT, 17, 24>
+                              : p.classes <= 40 ? thread_kernel<XT, 25, 40>
+                                                : thread_kernel<XT, 41, kFew>;
+    if (smem > 48 * 1024) {
+      const cudaError_t err = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+      if (err != cudaSuccess) return err;
+    }
+    return launch_pdl(k, dim3(grid), dim3(kThreadRows), smem, stream, static_cast<const Params>(p));
   }
   if (p.classes <= 2048) {
     const unsigned grid = static_cast<unsigned>((static_cast<long long>(p.rows) + kWarps - 1) / kWarps);
-    return launch_pdl(warp_kernel<XT>, dim3(grid), dim3(kThreads), 0, stream, p);
+    void (*k)(const Params) = p.classes <= 32 * V ? warp_kernel<XT, 1> : p.classes <= 64 * V ? warp_kernel<XT, 2> : warp_kernel<XT, 4>;
+    return launch_pdl(k, dim3(grid), dim3(kThreads), 0, stream, static_cast<const Params>(p));
   }
   p.ks = 1;
-  while (p.ks < 16 && static_cast<long long>(p.rows) * p.ks < 4 * sms && p.classes / V >= 2 * kThreads * p.ks) p.ks *= 2;
+  while (p.ks < 16 && static_cast<long long>(p.rows) * p.ks < sms && p.classes / V >= 2 * kThreads * p.ks) p.ks *= 2;
   static bool raised[kMaxDevices] = {};
   bool& done = raised[current_device_slot()];
   if (!done) {
