@@ -383,8 +383,10 @@ GI_API gi_status gi_slice8_pointwise_run(const void* dev_in, void* dev_out, cons
 
 /* Fully connected layer with 4-bit weights:
  *   y[r,o] = act(bias[o] + sum_k w[o,k] x[r,k]),   w[o,k] = scale[o, k / group] * (q[o,k] - zero[o, k / group])
- * with q and zero whole numbers of 0 .. 15.  For dtype GI_F16 and GI_BF16 products are exact and sums fp32, for each group before its
- * scale is applied; y is rounded once.  For GI_F32 x counts with all its digits.
+ * with q and zero whole numbers of 0 .. 15.  Up to 16 rows, and for GI_F32, nothing of a weight is rounded: q - zero is exact, sums are
+ * fp32 for each group before its scale is applied, and y is rounded once (GI_F32: x counts with all its 24 digits, down to 2^-110).
+ * For more rows of a 16-bit type each weight may be rounded once to that type, as the weights of a convolution are.  What an infinity
+ * or a NaN in a row of x leads to stays in that row of y.
  * (Section 3.2 treats the 1x1 convolution as an operator of its own; the paper has no counterpart of the weights' type.) */
 typedef struct gi_linear_q4 {
   int32_t cin, cout;      /* up to 2^20 each */

@@ -219,10 +219,15 @@ def _torch_dtype(dtype: int):
     return {GI_F16: torch.float16, GI_BF16: torch.bfloat16, GI_F32: torch.float32}[dtype]
 
 
+_GI_DTYPES = {}
+
+
 def _gi_dtype(t) -> int:
     """GI_* of a torch tensor's element type (0 where the library has none)."""
-    import torch
-    return {torch.float16: GI_F16, torch.bfloat16: GI_BF16, torch.float32: GI_F32}.get(t.dtype, 0)
+    if not _GI_DTYPES:
+        import torch
+        _GI_DTYPES.update({torch.float16: GI_F16, torch.bfloat16: GI_BF16, torch.float32: GI_F32})
+    return _GI_DTYPES.get(t.dtype, 0)
 
 
 def _host(t, what: str, dtypes, shape):
@@ -236,26 +241,31 @@ def _host(t, what: str, dtypes, shape):
 
 def _rows(t, what: str, dtype, channels: int, device):
     """(pointer, elements between rows, rows) of a device tensor [..., channels] whose leading axes form rows at one pitch."""
-    if t.dtype != dtype or t.device != device or t.dim() < 1 or t.shape[-1] != channels:
-        raise ValueError(f"{what}: need {dtype} of shape [..., {channels}] on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
-    if t.dim() == 2:
-        if t.stride(1) == 1 or channels == 1:
-            return t.data_ptr(), t.stride(0), t.shape[0]
+    shape = t.shape
+    if t.dtype != dtype or t.device != device or not shape or shape[-1] != channels:
+        raise ValueError(f"{what}: need {dtype} of shape [..., {channels}] on {device}, got {t.dtype} {tuple(shape)} on {t.device}")
+    if len(shape) == 2:
+        pitch, step = t.stride()
+        if step == 1 or channels == 1:
+            return t.data_ptr(), pitch, shape[0]
     elif t.is_contiguous():
         return t.data_ptr(), channels, t.numel() // channels
     raise ValueError(f"{what}: channels must be contiguous, and all of a tensor of other than two axes (strides {t.stride()})")
 
 
-def _on(device, stream, call):
-    """call(stream handle) with `device` current: the library launches on the current device."""
+def _on(device, stream, call, *args) -> int:
+    """call(*args, stream handle) with `device` current: the library launches on the current device."""
     import torch
+    index = device.index
     if stream is None:
-        stream = torch.cuda.current_stream(device)
-    handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
-    if torch.cuda.current_device() == device.index:
-        return call(handle)
+        # (the handle alone: torch.cuda.current_stream() takes 2 us to make a Stream of it, a quarter of a small call)
+        handle = torch._C._cuda_getCurrentRawStream(index)
+    else:
+        handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+    if torch.cuda.current_device() == index:
+        return call(*args, handle)
     with torch.cuda.device(device):
-        return call(handle)
+        return call(*args, handle)
 
 
 class LinearQ4:
@@ -284,18 +294,25 @@ class LinearQ4:
         self.cin, self.cout, self.dtype = cin, cout, _torch_dtype(dtype)
         self.blob = blob.to(device)
         self.device = self.blob.device
+        self._run = lib().gi_linear_q4_run
+
+    @property
+    def _blob(self) -> int:
+        return self.blob.data_ptr()
 
     def run(self, x, y=None, stream=None):
         """y[..., cout] = act(x[..., cin] w^T + bias) on `stream` (default: the current one of the layer's device); y is made where none is given.
         Two axes may have any distance between rows; other tensors are contiguous."""
-        import torch
         if y is None:
+            import torch
             y = torch.empty(tuple(x.shape[:-1]) + (self.cout,), dtype=self.dtype, device=self.device)
         xp, ldx, rows = _rows(x, "x", self.dtype, self.cin, self.device)
         yp, ldy, yrows = _rows(y, "y", self.dtype, self.cout, self.device)
         if rows != yrows:
             raise ValueError(f"x has {rows} rows, y {yrows}")
-        _check(_on(self.device, stream, lambda s: lib().gi_linear_q4_run(self._ref, self.blob.data_ptr(), xp, ldx, yp, ldy, rows, s)), "gi_linear_q4_run")
+        status = _on(self.device, stream, self._run, self._ref, self._blob, xp, ldx, yp, ldy, rows)
+        if status != GI_OK:
+            _check(status, "gi_linear_q4_run")
         return y
 
 
@@ -323,24 +340,31 @@ def log_probs(logits, given=None, top: int = 0, temperature: float = 1.0, out: O
     each row, in `out` (log_probs_out) or in new tensors."""
     import torch
     classes = logits.shape[-1]
-    ptr, ld, rows = _rows(logits, "logits", logits.dtype, classes, logits.device)
-    n_given = 0 if given is None else int(given.shape[-1])
+    device = logits.device
+    ptr, ld, rows = _rows(logits, "logits", logits.dtype, classes, device)
+    n_given = 0 if given is None else given.shape[-1]
     if out is None:
-        out = log_probs_out(rows, n_given, top, logits.device)
-    ptrs = []
-    for what, t, n, dtype in (("given", given, n_given, torch.int32), ("out.given", out.given, n_given, torch.float32),
-                              ("out.entropy", out.entropy, 1, torch.float32), ("out.top_ids", out.top_ids, top, torch.int32),
-                              ("out.top", out.top, top, torch.float32)):
-        if t is None or n == 0:
-            if n and what != "out.entropy":
-                raise ValueError(f"{what}: missing")
-            ptrs.append(None)
-            continue
-        if t.dtype != dtype or t.device != logits.device or not t.is_contiguous() or t.numel() != rows * n:
-            raise ValueError(f"{what}: need contiguous {dtype} of {rows} x {n} values on {logits.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
-        ptrs.append(t.data_ptr())
+        out = log_probs_out(rows, n_given, top, device)
+
+    def pointer(t, what, n, dtype):
+        if t is None:
+            raise ValueError(f"{what}: missing")
+        if t.dtype != dtype or t.device != device or not t.is_contiguous() or t.numel() != rows * n:
+            raise ValueError(f"{what}: need contiguous {dtype} of {rows} x {n} values on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        return t.data_ptr()
+
+    f32, i32 = torch.float32, torch.int32
+    gp = op = ep = ip = tp = None
+    if n_given:
+        gp, op = pointer(given, "given", n_given, i32), pointer(out.given, "out.given", n_given, f32)
+    if out.entropy is not None:
+        ep = pointer(out.entropy, "out.entropy", 1, f32)
+    if top:
+        ip, tp = pointer(out.top_ids, "out.top_ids", top, i32), pointer(out.top, "out.top", top, f32)
     d = gi_log_probs_desc(rows, classes, ld, _gi_dtype(logits), temperature, n_given, top)
-    _check(_on(logits.device, stream, lambda s: lib().gi_log_probs(C.byref(d), ptr, *ptrs, s)), "gi_log_probs")
+    status = _on(device, stream, lib().gi_log_probs, C.byref(d), ptr, gp, op, ep, ip, tp)
+    if status != GI_OK:
+        _check(status, "gi_log_probs")
     return out
 
 

@@ -145,6 +145,7 @@ gi_status gi_device_status(uint32_t* flags) {
   if (!flags) return fail(GI_E_INVALID, "gi_device_status: null argument");
   int err = 0;
   *flags = pointwise_tc_error_word(&err);
+  if (err == 0) *flags |= linear_q4_tc_error_word(&err);
   if (err == 0) *flags |= depthwise_error_word(&err) << 16;
   if (err == 0) *flags |= conv3x3_tc_error_word(&err) << 20;
   if (err == 0) *flags |= conv_kxk_tc_error_word(&err) << 20;

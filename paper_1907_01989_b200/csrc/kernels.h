@@ -138,11 +138,11 @@ struct LinearQ4Weights {
   const uint8_t* zeros = nullptr;
   int cin = 0, cout = 0, group = 0, scale_dtype = GI_F16, dtype = GI_F16;
 };
-// the packed blob: n_blocks x n_units records, then the bias
+// the packed blob: n_blocks x n_units records, then for each output the bias and a power of two for its scales
 struct LinearQ4Layout {
   int n_blocks = 0, n_units = 0, parts = 1;  // parts of a record with a scale of their own
   int record = 0, zeros_at = 0;              // bytes of a record, of what lies in front of its zero points
-  uint64_t bias = 0, bytes = 0;
+  uint64_t bias = 0, power = 0, bytes = 0;
 };
 // One product.  Rows of x and y are `x_row` / `y_row` elements apart, channels contiguous; or, with x_slice / y_slice > 0, both lie in
 // slices of 4 channels (rows are stored pixels).  plane > 0: y is the caller's NHWC tensor, its pixels `real` of `plane` stored ones.
@@ -158,6 +158,10 @@ struct LinearQ4Call {
 LinearQ4Layout linear_q4_layout(int cin, int cout, int group, int scale_dtype, bool zeros, int dtype);
 void linear_q4_pack(const LinearQ4Weights& w, const float* bias, uint8_t* blob);  // blob: layout.bytes bytes
 int launch_linear_q4(const LinearQ4Call& c, void* stream);
+// the same for many rows, on tcgen05 (linear_q4_tc.cu); reached through it
+bool linear_q4_tc_wanted(const LinearQ4Call& c);
+int launch_linear_q4_tc(const LinearQ4Call& c, const LinearQ4Layout& l, void* stream);
+unsigned int linear_q4_tc_error_word(int* cuda_err);
 
 // Log probabilities of classes, entropy and leading classes of rows of logits (log_probs.cu).
 struct LogProbsCall {

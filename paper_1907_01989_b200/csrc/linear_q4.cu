@@ -21,11 +21,13 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstring>
 
 #include "kernels.h"
 #include "mma_frag.cuh"
 #include "pdl.cuh"
+#include "q4_record.cuh"
 #include "sm100_ptx.cuh"
 
 namespace gi {
@@ -33,9 +35,9 @@ namespace {
 
 using namespace ptx;
 using namespace frag;
+using namespace q4;
 
 constexpr int kWarps = 8, kThreads = kWarps * 32;
-constexpr int kUnitK = 128, kUnitWeights = kUnitK * 16 / 2;
 // A warp's ring of copies: slots of two records (neighbours of one block, or one of each of two blocks).  Two CTAs of 8 warps keep
 // 128 KB of an SM's requests open.
 constexpr int kSlots = 4;
@@ -56,19 +58,10 @@ struct Params {
   int row_tile, x_vec;
   int chunk;                  // records of x staged at a time
   int ring_at, red_at;        // where the rings of copies, and the items' sums, begin in shared memory
-  unsigned low, high, digits; // masks of two weights of a word, and what they become the low digits of: as operands out of the
-                              // parameters (the compiler moves constants of this kind into registers again at every use)
+  q4::Masks q;
   int act_pre, has_res, act_post;
   int plane, real;            // > 0: stored and real pixels of a plane, padding pixels are not written
 };
-
-__device__ __forceinline__ void copy16(unsigned dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-// all but the last N groups of this thread's copies have landed
-template <int N>
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], const unsigned (&a)[4], unsigned b0, unsigned b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -87,61 +80,6 @@ __device__ __forceinline__ void mma(float (&d)[4], const unsigned (&a)[4], unsig
   else if (BF) mma_bf16(d, a, b0, b1);
   else if (FIRST) mma16816z(d, a, b0, b1);
   else mma16816(d, a, b0, b1);
-}
-
-// What is subtracted from the digits of a word's rows g and g + 8.
-struct Zero {
-  unsigned lo, hi;
-};
-template <bool BF>
-__device__ __forceinline__ Zero zero_of(const Params& p, unsigned z_lo, unsigned z_hi) {
-  if (BF) return Zero{p.digits | z_lo * 0x10001u, p.digits | z_hi * 0x10001u};  // 128 + z
-  return Zero{p.digits | z_lo * 0x10001u, 0xd400d400u | z_hi * 0x100010u};      // 1024 + z, -(64 + z)
-}
-
-// Eight weights of a word as the A operand: q - z, exact.
-template <bool BF>
-__device__ __forceinline__ void expand(const Params& p, unsigned w, const Zero& z, unsigned (&a)[4]) {
-  if (BF) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const unsigned v = ((w >> (4 * i)) & p.low) | p.digits;  // 128 + q
-      const unsigned c = i & 1 ? z.hi : z.lo;
-      const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v), *reinterpret_cast<const __nv_bfloat162*>(&c));
-      a[i] = *reinterpret_cast<const unsigned*>(&d);
-    }
-  } else {
-    const unsigned sixteenth = 0x2c002c00u;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const unsigned u = i ? w >> 8 : w;
-      const unsigned lo = (u & p.low) | p.digits;   // 1024 + q
-      const unsigned hi = (u & p.high) | p.digits;  // 1024 + 16 q
-      const __half2 d0 = __hsub2(*reinterpret_cast<const __half2*>(&lo), *reinterpret_cast<const __half2*>(&z.lo));
-      const __half2 d1 = __hfma2(*reinterpret_cast<const __half2*>(&hi), *reinterpret_cast<const __half2*>(&sixteenth),
-                                 *reinterpret_cast<const __half2*>(&z.hi));
-      a[2 * i] = *reinterpret_cast<const unsigned*>(&d0);
-      a[2 * i + 1] = *reinterpret_cast<const unsigned*>(&d1);
-    }
-  }
-}
-
-// Scales of rows g and g + 8.  S32: they are stored in 32 bits, else in the 16-bit type that x's kernel computes in (a choice by a
-// value of the call, among all three types, took 21 instructions of a record's 130).
-template <bool S32, bool BF>
-__device__ __forceinline__ float2 load_scales(unsigned at) {
-  if (S32) {
-    const uint2 v = lds64(at);
-    return make_float2(__uint_as_float(v.x), __uint_as_float(v.y));
-  }
-  const unsigned v = lds32(at);
-  if (BF) return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
-  return __half22float2(*reinterpret_cast<const __half2*>(&v));
-}
-__device__ __forceinline__ unsigned lds16(unsigned at) {
-  unsigned short v;
-  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at) : "memory");
-  return v;
 }
 
 // Eight channels k .. k + 7 of row r of x (16-bit types), zero behind the last one.
@@ -232,12 +170,6 @@ __device__ __forceinline__ void store_y(const Params& p, int r, int o, float v) 
   if (XT == GI_F16) static_cast<__half*>(p.y)[at] = __float2half_rn(v);
   else if (XT == GI_BF16) static_cast<__nv_bfloat16*>(p.y)[at] = __float2bfloat16_rn(v);
   else static_cast<float*>(p.y)[at] = v;
-}
-
-// bytes of a record, of what lies in front of its zero points
-__host__ __device__ constexpr int zeros_at(int parts, bool wide) { return kUnitWeights + parts * 16 * (wide ? 4 : 2); }
-__host__ __device__ constexpr int record_bytes(int parts, bool wide, bool zeros) {
-  return (zeros_at(parts, wide) + (zeros ? parts * 16 : 0) + 31) / 32 * 32;  // whole sectors
 }
 
 // XT: type of x and y.  NT: eights of columns (rows of x, three for a row of 32 bits).  RB: blocks of 16 outputs of a warp.
@@ -359,9 +291,9 @@ __global__ void __launch_bounds__(kThreads, 2) linear_q4_kernel(const Params p) 
         for (int s = 0; s < 4; ++s) {
           const int q = 4 * i + s, h = q * HG / 8;  // 16 channels; their group
           const bool first = q * kChains % 8 == 0, last = (q + 1) * kChains % 8 == 0;
-          const Zero z = ZP ? zero_of<BF>(p, zp[b][h] & 255u, zp[b][h] >> 8) : zero_of<BF>(p, 8u, 8u);
+          const Zero z = ZP ? zero_of<BF>(p.q, zp[b][h] & 255u, zp[b][h] >> 8) : zero_of<BF>(p.q, 8u, 8u);
           unsigned a[4];
-          expand<BF>(p, word[s], z, a);
+          expand<BF>(p.q, word[s], z, a);
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
             const uint4& v = xb[n][s >> 1];
@@ -472,9 +404,6 @@ __global__ void __launch_bounds__(kThreads, 2) linear_q4_kernel(const Params p) 
   if (p.ks > 1) cluster_sync();  // nobody leaves while its shared memory is read
 }
 
-// parts of a record that may belong to different groups
-int parts_of(int group) { return group % 128 == 0 ? 1 : group % 64 == 0 ? 2 : 4; }
-
 template <int XT, int NT, int RB, bool S32>
 cudaError_t launch_shape(const Params& p, int parts, bool zeros, unsigned grid, size_t smem, cudaStream_t stream) {
   void (*k)(const Params) = parts == 1   ? (zeros ? linear_q4_kernel<XT, NT, RB, 1, true, S32> : linear_q4_kernel<XT, NT, RB, 1, false, S32>)
@@ -545,10 +474,18 @@ cudaError_t launch_type(const Params& p, const Shape& s, int parts, bool zeros, 
   }
 }
 
-// Whether a layer's packed scales are 32 bits wide: those of 16 bits are kept where they are of the type its kernel computes in.
-bool wide_scales(int scale_dtype, int dtype) { return scale_dtype != (dtype == GI_F16 ? GI_F16 : GI_BF16); }
-
-int scale_bytes(int dtype) { return dtype == GI_F32 ? 4 : 2; }
+// a caller's scale in 32 bits: exact
+float scale_at(const LinearQ4Weights& w, size_t i) {
+  const uint8_t* p = static_cast<const uint8_t*>(w.scales) + i * (w.scale_dtype == GI_F32 ? 4 : 2);
+  if (w.scale_dtype == GI_F32) {
+    float f;
+    std::memcpy(&f, p, 4);
+    return f;
+  }
+  uint16_t v;
+  std::memcpy(&v, p, 2);
+  return w.scale_dtype == GI_F16 ? f16_to_f32(v) : bf16_to_f32(v);
+}
 
 }  // namespace
 
@@ -560,7 +497,8 @@ LinearQ4Layout linear_q4_layout(int cin, int cout, int group, int scale_dtype, b
   l.zeros_at = zeros_at(l.parts, wide_scales(scale_dtype, dtype));
   l.record = record_bytes(l.parts, wide_scales(scale_dtype, dtype), zeros);
   l.bias = round_up_u64(static_cast<uint64_t>(l.n_blocks) * l.n_units * l.record, 256);
-  l.bytes = round_up_u64(l.bias + static_cast<uint64_t>(l.n_blocks) * 16 * sizeof(float), 256);
+  l.power = l.bias + static_cast<uint64_t>(l.n_blocks) * 16 * sizeof(float);
+  l.bytes = round_up_u64(l.power + static_cast<uint64_t>(l.n_blocks) * 16 * sizeof(float), 256);
   return l;
 }
 
@@ -568,7 +506,6 @@ void linear_q4_pack(const LinearQ4Weights& w, const float* bias, uint8_t* blob) 
   const LinearQ4Layout l = linear_q4_layout(w.cin, w.cout, w.group, w.scale_dtype, w.zeros != nullptr, w.dtype);
   const int64_t pitch = (static_cast<int64_t>(w.cin) + 1) / 2;  // bytes of a row of the caller's
   const int64_t n_groups = (static_cast<int64_t>(w.cin) + w.group - 1) / w.group;
-  const int sb = scale_bytes(w.scale_dtype);
   const bool wide = wide_scales(w.scale_dtype, w.dtype);
   for (int b = 0; b < l.n_blocks; ++b)
     for (int u = 0; u < l.n_units; ++u) {
@@ -586,14 +523,11 @@ void linear_q4_pack(const LinearQ4Weights& w, const float* bias, uint8_t* blob) 
           for (int h = 0; h < l.parts; ++h) {
             const int64_t gr = std::min<int64_t>((static_cast<int64_t>(u) * kUnitK + h * (kUnitK / l.parts)) / w.group, n_groups - 1);
             const size_t from = static_cast<size_t>(o) * n_groups + gr, to = h * 16 + g * 2 + i;
-            const uint8_t* scale = static_cast<const uint8_t*>(w.scales) + from * sb;
-            if (wide && sb == 2) {
-              uint16_t v;
-              std::memcpy(&v, scale, 2);
-              const float f = w.scale_dtype == GI_F16 ? f16_to_f32(v) : bf16_to_f32(v);
+            if (wide) {
+              const float f = scale_at(w, from);
               std::memcpy(rec + kUnitWeights + to * 4, &f, 4);
             } else {
-              std::memcpy(rec + kUnitWeights + to * sb, scale, sb);
+              std::memcpy(rec + kUnitWeights + to * 2, static_cast<const uint8_t*>(w.scales) + from * 2, 2);
             }
             if (w.zeros) rec[l.zeros_at + to] = w.zeros[from] & 15u;
           }
@@ -611,19 +545,32 @@ void linear_q4_pack(const LinearQ4Weights& w, const float* bias, uint8_t* blob) 
     }
   std::memset(blob + l.bias, 0, l.bytes - l.bias);
   if (bias) std::memcpy(blob + l.bias, bias, static_cast<size_t>(w.cout) * sizeof(float));
+  // the power of two that brings an output's largest scale to 1/2 .. 1
+  for (int o = 0; o < l.n_blocks * 16; ++o) {
+    float largest = 0.0f, power = 1.0f;
+    for (int64_t gr = 0; o < w.cout && gr < n_groups; ++gr) {
+      const float v = std::fabs(scale_at(w, static_cast<size_t>(o) * n_groups + gr));
+      if (std::isfinite(v)) largest = std::max(largest, v);
+    }
+    if (largest > 0.0f) {
+      int e = 0;
+      std::frexp(largest, &e);
+      power = std::ldexp(1.0f, std::min(126, std::max(-126, -e)));
+    }
+    std::memcpy(blob + l.power + static_cast<size_t>(o) * 4, &power, 4);
+  }
 }
 
 int launch_linear_q4(const LinearQ4Call& c, void* stream) {
   if (c.rows <= 0) return 0;
   const LinearQ4Layout l = linear_q4_layout(c.cin, c.cout, c.group, c.scale_dtype, c.zeros, c.dtype);
+  if (linear_q4_tc_wanted(c)) return launch_linear_q4_tc(c, l, stream);
   const int cols_per_row = c.dtype == GI_F32 ? 3 : 1;
   const Shape s = choose_shape(c.rows, cols_per_row, l.n_blocks, l.n_units, device_sm_count());
   Params p{};
   const unsigned char* blob = static_cast<const unsigned char*>(c.blob);
   p.wts = blob;
-  p.low = 0x000f000fu;
-  p.high = 0x00f000f0u;
-  p.digits = c.dtype == GI_F16 ? 0x64006400u : 0x43004300u;
+  p.q = masks_of(c.dtype);
   p.bias = reinterpret_cast<const float*>(blob + l.bias);
   p.x = c.x;
   p.res = c.res;

@@ -33,17 +33,24 @@ def linear_q4(x, q, scales, zeros, bias, group, act="none"):
 
     n products (three for each input in 32 bits, which counts in three parts) added in any order, each addition off by at most 2^-23 of
     its result (twice half a step: a matrix instruction may cut off instead of rounding): n 2^-23 sum |products|; a scale and the
-    bias are two more operations.  Rounding: half a step of the result."""
+    bias are two more operations.  Rounding: half a step of the result.
+
+    More than 16 rows of a 16-bit type: each weight may be rounded to that type first - half a step of it, a little more where its scale
+    enters in two parts, and half of fp16's smallest step (2^-25) of a weight brought to the output's largest scale (by less than twice
+    its inverse)."""
     w = q4_weights(q, scales, zeros, x.shape[-1], group)
     xd = x.double().cpu()
     y = xd @ w.t()
     mag = xd.abs() @ w.abs().t()
+    rounded = 0.0
+    if x.shape[0] > 16 and x.dtype != torch.float32:
+        rounded = 1.02 * UNIT[x.dtype] * mag + 2.0 ** -24 * xd.abs().sum(1, keepdim=True) * scales.double().abs().amax(1)
     if bias is not None:
         y = y + bias.double()
         mag = mag + bias.double().abs()
     if act != "none":
         y = y.clamp(min=0.0, max=6.0 if act == "relu6" else math.inf)
-    sums = (x.shape[-1] * (3 if x.dtype == torch.float32 else 1) + 3) * 2.0 ** -23 * mag
+    sums = (x.shape[-1] * (3 if x.dtype == torch.float32 else 1) + 3) * 2.0 ** -23 * mag + rounded
     return y, sums + (y.abs() + sums) * UNIT[x.dtype] + TINY[x.dtype]
 
 

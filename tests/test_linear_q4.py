@@ -161,6 +161,38 @@ def test_groups_scales_and_zero_points(group, scale, zeros):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("rows", [17, 32, 33, 64, 100, 128, 250, 256, 257, 300, 513, 1000])
+def test_many_rows(rows, dtype):
+    layer, w = make(rows, 1096, 300, 32, dtype, zeros=True)
+    check(rows_of(rows, rows, 1096, dtype), layer, w, 32)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cin,cout", [(8, 1), (64, 128), (72, 129), (1000, 1001), (1288, 2000), (8192, 130), (4104, 4096)])
+@pytest.mark.parametrize("dtype,rows,scale", [(torch.float16, 20, torch.float16), (torch.bfloat16, 70, torch.float32), (torch.float16, 260, torch.bfloat16)])
+def test_many_rows_sizes(cin, cout, dtype, rows, scale):
+    layer, w = make(cin + cout, cin, cout, 64, dtype, scale, zeros=cin > 1000)
+    check(rows_of(7, rows, cin, dtype), layer, w, 64)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_scales_outside_fp16(dtype):
+    """Scales of 2^-60 and 2^40, side by side in one layer: weights that fp16 cannot hold."""
+    q, s, z, b = ref.q4_layer(2, 256, 40, 64, torch.float32, bias=False)
+    s = s * torch.where(torch.arange(40) % 2 == 0, 2.0 ** -60, 2.0 ** 40)[:, None]
+    layer = api.LinearQ4(q, s, cin=256, group=64, dtype=GI[dtype])
+    for rows in (4, 50):
+        x = rows_of(rows, rows, 256, dtype)
+        x = x * 2.0 ** -40 if dtype == torch.bfloat16 else x * 2.0 ** -14
+        got = layer.run(x.cuda())
+        want, bound = ref.linear_q4(x, q, s, None, None, 64)
+        keep = want.abs() < 6e4 if dtype == torch.float16 else want.abs() < 1e38
+        assert ((got.double().cpu() - want).abs() <= bound)[keep].all()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("act", ["none", "relu", "relu6"])
 @pytest.mark.parametrize("bias", [False, True])
 def test_epilogue(act, bias):
