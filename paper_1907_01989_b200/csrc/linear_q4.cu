@@ -42,7 +42,7 @@ constexpr int kWarps = 8, kThreads = kWarps * 32;
 // 128 KB of an SM's requests open.
 constexpr int kSlots = 4;
 constexpr int kSmemTwo = 113 * 1024;      // two CTAs on an SM
-constexpr int kSumBytes = 16000;          // most for the items' sums: with the rings (records of up to 1344 bytes) and one step of x inside that
+constexpr int kSumBytes = 16384;          // most for the items' sums: with the rings (records of up to 1344 bytes) and one step of x inside that
 
 struct Params {
   const unsigned char* wts;

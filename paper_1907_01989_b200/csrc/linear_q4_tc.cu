@@ -2,7 +2,7 @@
 // the weights' layout).
 //
 // Beyond some 16 rows the warp-level matrix instruction takes longer than the weights' bytes (8 cycles for 16 outputs x 8 rows x 16
-// channels).  Here a CTA computes 128 outputs x up to 256 rows: the weights are the A operand - eight warps, one for each block of 16
+// channels).  Here a CTA computes 128 outputs x up to 256 rows: the weights are the A operand - sixteen warps, two for each block of 16
 // outputs, expand the records that their own rings of copies bring, scale them and store them to shared memory in the swizzled
 // layout (rows of 64 channels = 128 bytes, 16-byte units exchanged by the row's number) - and the rows of x the B operand, copied by
 // one thread as tiles of the same layout.  One thread issues the products, 128 x N x 16 each; the sums stay in tensor memory until
@@ -30,7 +30,8 @@ namespace {
 using namespace ptx;
 using namespace q4;
 
-constexpr int kWorkers = 8;                    // warps that expand weights, and store the results
+constexpr int kBlocks = 8;                     // blocks of 16 outputs of a CTA
+constexpr int kWorkers = 2 * kBlocks;          // warps that expand weights - a block's two take the halves of its records - and store the results
 constexpr int kCopyWarp = kWorkers, kMmaWarp = kWorkers + 1;
 constexpr int kThreads = (kWorkers + 2) * 32;
 constexpr int kOuts = 128, kStageK = 64;       // outputs of a CTA, channels of a stage
@@ -116,6 +117,7 @@ template <bool BF, int HG, bool ZP, bool S32>
 __global__ void __launch_bounds__(kThreads, 1) linear_q4_tc_kernel(const __grid_constant__ CUtensorMap map, const Params p) {
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   constexpr int kZerosAt = zeros_at(HG, S32), kRecord = record_bytes(HG, S32, ZP), kBehind = kRecord - kUnitWeights;
+  constexpr int kSlot = 512 + kBehind;  // half a record's weights, and what lies behind them
   Header* hdr = reinterpret_cast<Header*>(smem_raw);
   volatile unsigned* abort_flag = &hdr->abort;
   const unsigned base = smem_u32(smem_raw), st0 = base + kHeader;
@@ -129,7 +131,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_q4_tc_kernel(const __grid_
   if (threadIdx.x == 0) {
     prefetch_tensormap(&map);
     for (int i = 0; i < p.stages; ++i) {
-      mbar_init(full_a + i * 8, kWorkers);
+      mbar_init(full_a + i * 8, kBlocks);
       mbar_init(full_b + i * 8, 1);
       mbar_init(empty + i * 8, 1);
     }
@@ -147,79 +149,77 @@ __global__ void __launch_bounds__(kThreads, 1) linear_q4_tc_kernel(const __grid_
   int asked = 0;  // copies of x asked for (the copying thread)
 
   if (warp < kWorkers) {
-    const int block = min(mt * kWorkers + warp, p.n_blocks - 1), g = lane >> 2, t = lane & 3;
-    const unsigned ring = st0 + p.stages * stage_bytes + warp * (kRing * kRecord);
+    const int half = warp / kBlocks, bl = warp % kBlocks;  // of a record; of the CTA's blocks
+    const int block = min(mt * kBlocks + bl, p.n_blocks - 1), g = lane >> 2, t = lane & 3, odd = g & 1;
+    const unsigned ring = st0 + p.stages * stage_bytes + warp * (kRing * kSlot);
     const unsigned char* next = p.wts + (static_cast<size_t>(block) * p.n_units + ua) * kRecord;
-    if (lane == 0) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(next), "r"(min(kRing, ub - ua) * kRecord) : "memory");
+    if (lane == 0 && half == 0) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(next), "r"(min(kRing, ub - ua) * kRecord) : "memory");
     next += lane * 16;
     pdl_wait();
     const float power_lo = p.power[block * 16 + g], power_hi = p.power[block * 16 + g + 8];
     auto request = [&](unsigned slot) {
-      copy16(slot + lane * 16, next);
-      copy16(slot + lane * 16 + 512, next + 512);
-      if (lane * 16 < kBehind) copy16(slot + lane * 16 + 1024, next + 1024);
+      copy16(slot + lane * 16, next + half * 512);
+      if (lane * 16 < kBehind) copy16(slot + 512 + lane * 16, next + kUnitWeights);
       next += kRecord;
     };
 #pragma unroll
     for (int j = 0; j < kRing; ++j) {
-      if (j < ub - ua) request(ring + j * kRecord);
+      if (j < ub - ua) request(ring + j * kSlot);
       copies_commit();
     }
     unsigned from = ring;
-    int stage = 0, phase = 1;  // (the first round finds its stages empty)
-    bool good = true;
-    for (int u = ua; u < ub && good; ++u) {
+    int stage = half, phase = 1;  // every second stage (the first round finds them empty)
+    for (int u = ua; u < ub; ++u) {
       copies_wait<kRing - 1>();
       __syncwarp();
-      const uint4 w[2] = {lds128(from + lane * 16), lds128(from + lane * 16 + 512)};
-      float2 f[HG];
-      unsigned zp[HG];
+      const uint4 w = lds128(from + lane * 16);
+      // Rows of odd numbers begin with their second 32 channels: the two rows that a quarter of a warp stores at a time then lie in
+      // different banks.
+      const unsigned word[4] = {odd ? w.z : w.x, odd ? w.w : w.y, odd ? w.x : w.z, odd ? w.y : w.w};
+      float2 f[2];
+      unsigned zp[2];
 #pragma unroll
-      for (int h = 0; h < HG; ++h) {
-        f[h] = load_scales<S32, BF>(from + kUnitWeights + (h * 8 + g) * (S32 ? 8 : 4));
-        if (ZP) zp[h] = lds16(from + kZerosAt + (h * 8 + g) * 2);
+      for (int h = 0; h < 2; ++h) {  // 32 channels: one group
+        const int part = HG == 4 ? 2 * half + (h ^ odd) : HG == 2 ? half : 0;
+        f[h] = load_scales<S32, BF>(from + 512 + (part * 8 + g) * (S32 ? 8 : 4));
+        if (ZP) zp[h] = lds16(from + 512 + kZerosAt - kUnitWeights + (part * 8 + g) * 2);
       }
       __syncwarp();
       if (u + kRing < ub) request(from);
       copies_commit();
-      from = from == ring + (kRing - 1) * kRecord ? ring : from + kRecord;
+      from = from == ring + (kRing - 1) * kSlot ? ring : from + kSlot;
+      uint4 out[2][2];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {  // 64 channels: a stage
-        const unsigned word[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-        uint4 out[2][2];
+      for (int h = 0; h < 2; ++h) {
+        const Zero z = ZP ? zero_of<BF>(p.q, zp[h] & 255u, zp[h] >> 8) : zero_of<BF>(p.q, 8u, 8u);
+        unsigned s0, s1, r0, r1, a[2][4];
+        halves<BF>(f[h].x * power_lo, s0, r0);
+        halves<BF>(f[h].y * power_hi, s1, r1);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {  // 32 channels: one group
-          const int part = (2 * i + h) * HG / 4;
-          const Zero z = ZP ? zero_of<BF>(p.q, zp[part] & 255u, zp[part] >> 8) : zero_of<BF>(p.q, 8u, 8u);
-          unsigned s0, s1, r0, r1, a[2][4];
-          halves<BF>(f[part].x * power_lo, s0, r0);
-          halves<BF>(f[part].y * power_hi, s1, r1);
+        for (int s = 0; s < 2; ++s) {
+          expand<BF>(p.q, word[2 * h + s], z, a[s]);
 #pragma unroll
-          for (int s = 0; s < 2; ++s) {
-            expand<BF>(p.q, word[2 * h + s], z, a[s]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const unsigned sc = e & 1 ? s1 : s0, rest = e & 1 ? r1 : r0;
-              a[s][e] = S32 ? fma<BF>(a[s][e], sc, mul<BF>(a[s][e], rest)) : mul<BF>(a[s][e], sc);
-            }
+          for (int e = 0; e < 4; ++e) {
+            const unsigned sc = e & 1 ? s1 : s0, rest = e & 1 ? r1 : r0;
+            a[s][e] = S32 ? fma<BF>(a[s][e], sc, mul<BF>(a[s][e], rest)) : mul<BF>(a[s][e], sc);
           }
-          out[h][0] = make_uint4(a[0][0], a[0][2], a[1][0], a[1][2]);
-          out[h][1] = make_uint4(a[0][1], a[0][3], a[1][1], a[1][3]);
         }
-        good = mbar_wait_warp(empty + stage * 8, phase, abort_flag, kWaitNs, &g_q4_tc_error, kErrWork);
-        if (!good) break;
-        const unsigned row = st0 + stage * stage_bytes + (warp * 16 + g) * 128;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const unsigned at = static_cast<unsigned>((4 * h + t) ^ g) << 4;
-          sts128(row + at, out[h][0].x, out[h][0].y, out[h][0].z, out[h][0].w);
-          sts128(row + 8 * 128 + at, out[h][1].x, out[h][1].y, out[h][1].z, out[h][1].w);
-        }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // visible to the tensor core
-        __syncwarp();
-        if (lane == 0) mbar_arrive(full_a + stage * 8);
-        if (++stage == p.stages) stage = 0, phase ^= 1;
+        out[h][0] = make_uint4(a[0][0], a[0][2], a[1][0], a[1][2]);
+        out[h][1] = make_uint4(a[0][1], a[0][3], a[1][1], a[1][3]);
       }
+      if (!mbar_wait_warp(empty + stage * 8, phase, abort_flag, kWaitNs, &g_q4_tc_error, kErrWork)) break;
+      const unsigned row = st0 + stage * stage_bytes + (bl * 16 + g) * 128;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const unsigned at = static_cast<unsigned>((4 * (h ^ odd) + t) ^ g) << 4;
+        sts128(row + at, out[h][0].x, out[h][0].y, out[h][0].z, out[h][0].w);
+        sts128(row + 8 * 128 + at, out[h][1].x, out[h][1].y, out[h][1].z, out[h][1].w);
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // visible to the tensor core
+      __syncwarp();
+      if (lane == 0) mbar_arrive(full_a + stage * 8);
+      stage += 2;
+      if (stage >= p.stages) stage -= p.stages, phase ^= 1;
     }
     copies_wait<0>();
   } else if (warp == kCopyWarp) {
@@ -277,7 +277,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_q4_tc_kernel(const __grid_
     const bool real = o < p.cout;
     const float inverse = real ? 1.0f / p.power[o] : 0.0f, bias = real ? p.bias[o] : 0.0f;
     float* sums = reinterpret_cast<float*>(smem_raw + kHeader);  // [row][output]: the stages' place
-    for (int c = (warp >> 2) * 16; c < p.n; c += 32) {
+    for (int c = (warp >> 2) * 16; c < p.n; c += kWorkers / 4 * 16) {
       unsigned v[16];
       tmem_ld16(tmem + (static_cast<unsigned>((warp & 3) * 32) << 16) + c, v);
       tmem_ld_wait16(v);
@@ -299,16 +299,30 @@ __global__ void __launch_bounds__(kThreads, 1) linear_q4_tc_kernel(const __grid_
     if (!give_up) {
       const unsigned sums = st0;
       const int total = min(p.n, p.rows - row0) * kOuts;
-      for (int i = threadIdx.x + rank * kThreads; i < total; i += kThreads * p.ks) {
-        const int o = mt * kOuts + (i & (kOuts - 1));
-        if (o >= p.cout) continue;
-        float v = 0.0f;
-        for (int k = 0; k < p.ks; ++k) {
-          float s;
-          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(s) : "r"(mapa_shared(sums + i * 4, k)) : "memory");
-          v += s;
-        }
-        store_y<BF>(p, row0 + i / kOuts, o, fmaf(v, 1.0f / p.power[o], p.bias[o]));
+      for (int i = (threadIdx.x + rank * kThreads) * 4; i < total; i += kThreads * p.ks * 4) {
+        const int o = mt * kOuts + (i & (kOuts - 1)), row = row0 + i / kOuts;
+        float4 part[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (k < p.ks) {
+            const unsigned from = mapa_shared(sums + i * 4, k);
+            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                         : "=f"(part[k].x), "=f"(part[k].y), "=f"(part[k].z), "=f"(part[k].w)
+                         : "r"(from)
+                         : "memory");
+          }
+        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (k < p.ks) {
+            v[0] += part[k].x;
+            v[1] += part[k].y;
+            v[2] += part[k].z;
+            v[3] += part[k].w;
+          }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (o + j < p.cout) store_y<BF>(p, row, o + j, fmaf(v[j], 1.0f / p.power[o + j], p.bias[o + j]));
       }
     }
     cluster_sync();  // nobody leaves while its shared memory is read
@@ -344,18 +358,20 @@ int launch_linear_q4_tc(const LinearQ4Call& c, const LinearQ4Layout& l, void* st
   p.n_units = l.n_units;
   p.act = c.ep.act_pre;
   p.q = masks_of(c.dtype);
-  p.m_tiles = (l.n_blocks + kWorkers - 1) / kWorkers;
-  const long long n_tiles = (static_cast<long long>(c.rows) + 255) / 256;
-  p.n = static_cast<int>((c.rows + n_tiles - 1) / n_tiles + 15) / 16 * 16;
-  const long long row_tiles = (static_cast<long long>(c.rows) + p.n - 1) / p.n;
-  p.tmem_cols = 32;
-  while (p.tmem_cols < p.n) p.tmem_cols *= 2;
-  const int rings = kWorkers * kRing * l.record, stage = kABytes + p.n * kStageK * 2;
-  p.stages = std::min(kMaxStages, (kSmem - kHeader - rings) / stage);
-  // CTAs that share a sum: as many as fill the GPU, each with 512 channels or more
+  p.m_tiles = (l.n_blocks + kBlocks - 1) / kBlocks;
+  // Tiles of up to 256 rows, which expand the weights once; CTAs that share a sum, as many as fill the GPU, each with 512 channels or
+  // more; where even that leaves SMs idle, smaller tiles of rows (256 rows 1280 -> 1001 17 us with 16 CTAs).
   const int sms = device_sm_count();
+  long long row_tiles = (static_cast<long long>(c.rows) + 255) / 256;
   p.ks = 1;
   while (p.ks < 8 && p.m_tiles * row_tiles * p.ks * 2 <= sms && p.n_units >= 8 * p.ks) p.ks *= 2;
+  while (p.m_tiles * row_tiles * p.ks * 2 <= sms && c.rows > 32 * row_tiles) row_tiles *= 2;
+  p.n = static_cast<int>((c.rows + row_tiles - 1) / row_tiles + 15) / 16 * 16;
+  row_tiles = (static_cast<long long>(c.rows) + p.n - 1) / p.n;
+  p.tmem_cols = 32;
+  while (p.tmem_cols < p.n) p.tmem_cols *= 2;
+  const int rings = kWorkers * kRing * (l.record - kUnitWeights / 2), stage = kABytes + p.n * kStageK * 2;
+  p.stages = std::min(kMaxStages, (kSmem - kHeader - rings) / stage);
   const size_t smem = kHeader + std::max<size_t>(static_cast<size_t>(p.stages) * stage + rings, p.ks > 1 ? static_cast<size_t>(p.n) * kOuts * 4 : 0);
   const long long grid = p.m_tiles * row_tiles * p.ks;
   if (grid > 0x7fffffffll || p.stages < 2 || smem > static_cast<size_t>(kSmem)) return static_cast<int>(cudaErrorInvalidConfiguration);
