@@ -64,7 +64,8 @@ enum {
 };
 
 enum { GI_F16 = 1, GI_F32 = 2 };   /* storage type of activations (and of NHWC inputs/outputs) */
-enum { GI_BF16 = 3 };              /* operators on rows (gi_linear_q4_run, gi_log_probs) only */
+enum { GI_BF16 = 3 };              /* operators on rows (gi_linear_q4_run, gi_log_probs), and scales of GI_Q4 weights */
+enum { GI_Q4 = 4 };                /* weights of a 1x1 convolution: 4 bits each, with a scale for each group (gi_q4_weights) */
 enum { GI_NHWC = 0, GI_PHWC4 = 1 }; /* layout of a caller-visible tensor */
 
 enum {
@@ -135,9 +136,20 @@ enum {
  * weights: host pointer, [cout][kh][kw][cin] for CONV2D, [1][kh][kw][c] for DEPTHWISE_CONV2D,
  * of type weight_dtype (GI_F32 or GI_F16); bias: host pointer to cout floats or NULL.  Both
  * are copied by gi_add_op; the caller may free them as soon as it returns.
+ * GI_Q4 (CONV2D with a 1x1 kernel): `weights` points at a gi_q4_weights, whose arrays are copied as well.  A plain 1x1 convolution
+ * of few pixels - at most 16 stored ones, as a classifier behind the pooling has - then reads a quarter of the bytes (GI_PW_AUTO,
+ * fp16 storage); everywhere else the weights are expanded by gi_compile, and rounded to fp16 as any others.
  * Unused fields must be zero.  inputs[1] is used by GI_OP_ADD and GI_OP_CONCAT only (elsewhere -1 or 0); there -1
  * means "no second input": the operator is then an identity, which gi_compile removes (Section 3.1).
  */
+typedef struct gi_q4_weights {
+  const uint8_t* q;       /* [cout][(cin + 1) / 2]: whole numbers of 0 .. 15, two a byte, the even input channel in the low half */
+  const void* scales;     /* [cout][ceil(cin / group)] of type scale_dtype: w = scale * (q - zero) */
+  const uint8_t* zeros;   /* the same number of zero points, 0 .. 15; NULL: 8 everywhere */
+  int32_t scale_dtype;    /* GI_F16, GI_BF16 or GI_F32 */
+  int32_t group;          /* input channels that share a scale: a multiple of 32 */
+} gi_q4_weights;
+
 typedef struct gi_op_desc {
   int32_t kind;
   gi_tensor inputs[2];
@@ -228,7 +240,8 @@ enum {
   GI_KERNEL_POINTWISE_CHAIN = 17,     /* this op (1x1) and the next one (1x1) as one kernel; both outputs are stored */
   GI_KERNEL_BLOCK_MMA = 18,           /* gi_exec_launch only: a depthwise 3x3 op with the ops around it as one kernel */
   GI_KERNEL_POINTWISE_MMA = 19,       /* gi_exec_launch only: 1x1 convolution for launches bound by latency (and the layout conversion behind it) */
-  GI_KERNEL_CONV_MMA = 20             /* gi_exec_launch only: k x k convolution with few channels, or a whole fire module */
+  GI_KERNEL_CONV_MMA = 20,            /* gi_exec_launch only: k x k convolution with few channels, or a whole fire module */
+  GI_KERNEL_LINEAR_Q4 = 21            /* 1x1 convolution of few pixels with 4-bit weights */
 };
 
 /* ---- graph construction (Section 3.1, "Initialization": the sub-graph given to the GPU backend) ---- */

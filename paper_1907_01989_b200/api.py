@@ -19,7 +19,7 @@ LIB_PATH = os.path.join(_HERE, "libgi.so")
 
 GI_OK = 0
 GI_E_INVALID, GI_E_UNSUPPORTED, GI_E_NOMEM, GI_E_CUDA, GI_E_STATE, GI_E_ARENA = -1, -2, -3, -4, -5, -6
-GI_F16, GI_F32, GI_BF16 = 1, 2, 3  # GI_BF16: operators on rows only
+GI_F16, GI_F32, GI_BF16, GI_Q4 = 1, 2, 3, 4  # GI_BF16: operators on rows, scales; GI_Q4: weights of a 1x1 convolution
 GI_NHWC, GI_PHWC4 = 0, 1
 GI_OP_CONV2D, GI_OP_DEPTHWISE_CONV2D, GI_OP_ADD, GI_OP_ACTIVATION, GI_OP_GLOBAL_AVG_POOL, GI_OP_RESIZE_BILINEAR = 1, 2, 3, 4, 5, 6
 GI_OP_CONCAT = 7
@@ -31,7 +31,7 @@ GI_XOP_AUTO, GI_XOP_OFF, GI_XOP_ON, GI_XOP_CHAIN = 0, 1, 2, 3
 GI_STATIC_ARENA_BYTES = 16 << 20
 GI_MAX_TOP = 32
 KERNEL_NAMES = {1: "pack", 2: "unpack", 3: "conv_simt", 4: "pointwise_tc", 5: "depthwise", 6: "eltwise", 7: "pool",
-                8: "resize", 9: "conv3x3_tc", 10: "pointwise_ts", 11: "depthwise_pointwise", 12: "none", 13: "concat", 14: "conv_tc", 15: "inverted_residual", 16: "pointwise_mm", 17: "pointwise_chain", 18: "block_mma", 19: "pointwise_mma", 20: "conv_mma"}
+                8: "resize", 9: "conv3x3_tc", 10: "pointwise_ts", 11: "depthwise_pointwise", 12: "none", 13: "concat", 14: "conv_tc", 15: "inverted_residual", 16: "pointwise_mm", 17: "pointwise_chain", 18: "block_mma", 19: "pointwise_mma", 20: "conv_mma", 21: "linear_q4"}
 
 _KIND = {wl.CONV2D: GI_OP_CONV2D, wl.DEPTHWISE: GI_OP_DEPTHWISE_CONV2D, wl.ADD: GI_OP_ADD,
          wl.ACTIVATION: GI_OP_ACTIVATION, wl.GLOBAL_AVG_POOL: GI_OP_GLOBAL_AVG_POOL,
@@ -46,6 +46,10 @@ class gi_op_desc(C.Structure):
                 ("cout", C.c_int32), ("act", C.c_int32), ("out_h", C.c_int32), ("out_w", C.c_int32),
                 ("align_corners", C.c_int32), ("weight_dtype", C.c_int32), ("weights", C.c_void_p),
                 ("bias", C.c_void_p)]
+
+
+class gi_q4_weights(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("scales", C.c_void_p), ("zeros", C.c_void_p), ("scale_dtype", C.c_int32), ("group", C.c_int32)]
 
 
 class gi_compile_options(C.Structure):
@@ -423,10 +427,19 @@ def graph_from_spec(spec: wl.GraphSpec, storage: int = GI_F16, io_layout: int = 
             d.dilation_h, d.dilation_w = op.dilation
             d.pad_t, d.pad_l, d.pad_b, d.pad_r = op.pads
             d.cout = op.cout
-            w = np.ascontiguousarray(op.weights, dtype=np.float32)
-            keep.append(w)
-            d.weight_dtype = GI_F32
-            d.weights = w.ctypes.data
+            if op.q4 is not None:
+                q, s = np.ascontiguousarray(op.q4.q, dtype=np.uint8), np.ascontiguousarray(op.q4.scales)
+                z = None if op.q4.zeros is None else np.ascontiguousarray(op.q4.zeros, dtype=np.uint8)
+                kind = {np.dtype(np.float16): GI_F16, np.dtype(np.float32): GI_F32}[s.dtype]
+                w4 = gi_q4_weights(q.ctypes.data, s.ctypes.data, None if z is None else z.ctypes.data, kind, op.q4.group)
+                keep += [q, s, z, w4]
+                d.weight_dtype = GI_Q4
+                d.weights = C.addressof(w4)
+            else:
+                w = np.ascontiguousarray(op.weights, dtype=np.float32)
+                keep.append(w)
+                d.weight_dtype = GI_F32
+                d.weights = w.ctypes.data
             if op.bias is not None:
                 b = np.ascontiguousarray(op.bias, dtype=np.float32)
                 keep.append(b)

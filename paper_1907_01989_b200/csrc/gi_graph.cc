@@ -68,6 +68,40 @@ float bf16_to_f32(uint16_t h) {
   return v;
 }
 
+// The weights of a 1x1 convolution in 4 bits: copied as they are, and expanded into node->weights.
+static gi_status take_q4(const gi_q4_weights* w, int cin, int cout, OpNode* node) {
+  if (!w->q || !w->scales) return fail(GI_E_INVALID, "gi_add_op: 4-bit weights without values or scales");
+  if (w->scale_dtype != GI_F16 && w->scale_dtype != GI_BF16 && w->scale_dtype != GI_F32)
+    return fail(GI_E_INVALID, "gi_add_op: scale_dtype must be GI_F16, GI_BF16 or GI_F32");
+  if (w->group <= 0) return fail(GI_E_INVALID, "gi_add_op: group must be positive");
+  if (w->group % 32 != 0 || cin > (1 << 20) || cout > (1 << 20)) return fail(GI_E_UNSUPPORTED, "gi_add_op: group must be a multiple of 32, cin and cout at most 2^20");
+  const size_t pitch = (static_cast<size_t>(cin) + 1) / 2, groups = (static_cast<size_t>(cin) + w->group - 1) / w->group, n = groups * cout;
+  const size_t sb = w->scale_dtype == GI_F32 ? 4 : 2;
+  for (size_t i = 0; w->zeros && i < n; ++i)
+    if (w->zeros[i] > 15) return fail(GI_E_INVALID, "gi_add_op: zero point above 15");
+  node->q4.assign(w->q, w->q + pitch * cout);
+  node->q4_scales.assign(static_cast<const uint8_t*>(w->scales), static_cast<const uint8_t*>(w->scales) + n * sb);
+  if (w->zeros) node->q4_zeros.assign(w->zeros, w->zeros + n);
+  node->q4_group = w->group;
+  node->q4_scale_dtype = w->scale_dtype;
+  node->weights.resize(static_cast<size_t>(cout) * cin);
+  for (int o = 0; o < cout; ++o)
+    for (int k = 0; k < cin; ++k) {
+      const size_t at = o * groups + k / w->group;
+      float s;
+      if (sb == 4) {
+        std::memcpy(&s, node->q4_scales.data() + at * 4, 4);
+      } else {
+        uint16_t h;
+        std::memcpy(&h, node->q4_scales.data() + at * 2, 2);
+        s = w->scale_dtype == GI_F16 ? f16_to_f32(h) : bf16_to_f32(h);
+      }
+      const int q = node->q4[o * pitch + k / 2] >> (k % 2 * 4) & 15, z = w->zeros ? node->q4_zeros[at] : 8;
+      node->weights[static_cast<size_t>(o) * cin + k] = s * static_cast<float>(q - z);
+    }
+  return GI_OK;
+}
+
 static int conv_out(int in, int k, int stride, int dil, int p0, int p1) {
   const int span = (k - 1) * dil + 1;
   const int padded = in + p0 + p1;
@@ -187,8 +221,10 @@ static gi_status add_op_checked(gi_graph* g, const gi_op_desc* desc, gi_tensor* 
       if (desc->pad_t < 0 || desc->pad_l < 0 || desc->pad_b < 0 || desc->pad_r < 0)
         return fail(GI_E_INVALID, "gi_add_op: negative padding");
       if (!desc->weights) return fail(GI_E_INVALID, "gi_add_op: convolution without weights");
-      if (desc->weight_dtype != GI_F32 && desc->weight_dtype != GI_F16)
-        return fail(GI_E_INVALID, "gi_add_op: weight_dtype must be GI_F32 or GI_F16");
+      if (desc->weight_dtype != GI_F32 && desc->weight_dtype != GI_F16 && desc->weight_dtype != GI_Q4)
+        return fail(GI_E_INVALID, "gi_add_op: weight_dtype must be GI_F32, GI_F16 or GI_Q4");
+      if (desc->weight_dtype == GI_Q4 && (dwise || desc->kh != 1))
+        return fail(GI_E_UNSUPPORTED, "gi_add_op: 4-bit weights are for 1x1 convolutions");
       const int cout = dwise ? in.c : desc->cout;
       if (cout <= 0) return fail(GI_E_INVALID, "gi_add_op: cout must be positive");
       o.h = conv_out(in.h, desc->kh, desc->stride_h, desc->dilation_h, desc->pad_t, desc->pad_b);
@@ -198,7 +234,10 @@ static gi_status add_op_checked(gi_graph* g, const gi_op_desc* desc, gi_tensor* 
       node.d.cout = cout;
       const size_t nw = static_cast<size_t>(dwise ? 1 : cout) * desc->kh * desc->kw * in.c;
       node.weights.resize(nw);
-      if (desc->weight_dtype == GI_F32) {
+      if (desc->weight_dtype == GI_Q4) {
+        const gi_status st = take_q4(static_cast<const gi_q4_weights*>(desc->weights), in.c, cout, &node);
+        if (st != GI_OK) return st;
+      } else if (desc->weight_dtype == GI_F32) {
         std::memcpy(node.weights.data(), desc->weights, nw * sizeof(float));
       } else {
         const uint16_t* h = static_cast<const uint16_t*>(desc->weights);

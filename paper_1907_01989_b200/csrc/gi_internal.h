@@ -20,6 +20,9 @@ struct OpNode {
   gi_op_desc d{};             // weights/bias pointers are cleared; the data lives below
   std::vector<float> weights; // fp32 copy, [cout][kh][kw][cin] (depthwise [kh][kw][c])
   std::vector<float> bias;    // cout floats, zeros if none was given
+  // 4-bit weights as the caller gave them (`weights` holds them expanded); no group: not 4-bit
+  std::vector<uint8_t> q4, q4_scales, q4_zeros;
+  int q4_group = 0, q4_scale_dtype = 0;
   int output = -1;
 };
 
@@ -112,6 +115,7 @@ struct LaunchRec {
   // one's behind it, `ep2` the projection's; Cmid / Co2, stride, pads and (Ho, Wo) as above; (H, W) the depthwise input
   BlockCfg block;
   int split_bias = 1;  // the first operator's biases can be written as fp16 parts (bias_split.h)
+  int q4_group = 0, q4_scale_dtype = 0, q4_zeros = 0;  // 4-bit weights
   int nhwc_out = 0;  // the kernel writes the caller's NHWC output itself
   // a launch that reads the caller's NHWC input while it writes a caller's output: arena bytes for a copy of the input where the
   // caller handed over overlapping buffers, and the sizes of both

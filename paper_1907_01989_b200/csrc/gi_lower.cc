@@ -54,6 +54,10 @@ static Loc loc_of(const gi_exec* e, int t) {
   return l;
 }
 
+// Stored pixels up to which a 1x1 convolution runs on its 4-bit weights: the kernel's sixteen rows, all of a batch of 8 behind a
+// pooling (a stored plane holds two pixels at least).  With more the fp16 kernels share a weight's bytes among enough pixels.
+constexpr long long kQ4Pixels = 16;
+
 // Weights of the CUDA-core convolution kernel: float W[group][tap][in_slice][32 co][4 ci],
 // a group being 8 consecutive output slices; entries beyond Cin / Cout are zero.
 static void pack_conv_simt(const OpNode& op, int cin, int storage, std::vector<uint8_t>* blob, LaunchRec* r) {
@@ -822,8 +826,11 @@ static gi_status lower_pass(const gi_graph& g, gi_exec* e, bool grouped, bool pa
           // them got faster - the CTA-pair kernel on 960 -> 160, the lane-per-pixel kernel's drain on 160 -> 960; now
           // three kernels per block win: 1.450 ms against 1.469 ms with the blocks fused (55 us each, bound by their own
           // instruction stream).
+          // 4-bit weights of few pixels: read as they are
+          const bool q4 = op.q4_group > 0 && pointwise && tc && e->opt.pointwise == GI_PW_AUTO &&
+                          static_cast<long long>(e->batch) * plane_pixels(din->h, din->w) <= kQ4Pixels;
           long long ir_units = 0;
-          if (pointwise && tc && e->opt.fuse && e->opt.cross_op != GI_XOP_OFF && block_follows(g, e, i)) {
+          if (pointwise && tc && !q4 && e->opt.fuse && e->opt.cross_op != GI_XOP_OFF && block_follows(g, e, i)) {
             const FusedOp& fd = e->ops[i + 1];
             const FusedOp& fp = e->ops[i + 2];
             const OpNode& dwn = g.ops[fd.graph_op];
@@ -867,7 +874,7 @@ static gi_status lower_pass(const gi_graph& g, gi_exec* e, bool grouped, bool pa
           // planes with at most 64 channels in the middle and at least two tiles per SM.
           const long long pc_tiles = (m_px_all_for_mm(e, din) + 127) / 128;
           const bool chain_auto = din->h * din->w > 64 && din->h * din->w <= 256 && op.d.cout <= 64 && din->c >= 192 && pc_tiles >= 2 * 148;
-          if (pointwise && tc && e->opt.fuse && (e->opt.cross_op == GI_XOP_CHAIN || (e->opt.cross_op == GI_XOP_AUTO && chain_auto)) &&
+          if (pointwise && tc && !q4 && e->opt.fuse && (e->opt.cross_op == GI_XOP_CHAIN || (e->opt.cross_op == GI_XOP_AUTO && chain_auto)) &&
               chain_follows(g, e, i) && !(grouped && group_of(e, i + 1)) &&
               pointwise_chain_supported(din->c, op.d.cout, g.ops[e->ops[i + 1].graph_op].d.cout, f.residual >= 0)) {
             const FusedOp& fb = e->ops[i + 1];
@@ -914,8 +921,28 @@ static gi_status lower_pass(const gi_graph& g, gi_exec* e, bool grouped, bool pa
               pair_tab = lc->kernel == GI_KERNEL_POINTWISE_TC;
             }
           }
-          if (grouped && pointwise && tc && e->opt.fuse && e->opt.pointwise == GI_PW_AUTO && e->opt.cross_op == GI_XOP_AUTO &&
-              pointwise_mma_wanted(r)) {
+          if (q4) {
+            r.kernel = GI_KERNEL_LINEAR_Q4;
+            r.ep = one_activation(r.ep);
+            r.q4_group = op.q4_group;
+            r.q4_scale_dtype = op.q4_scale_dtype;
+            r.q4_zeros = op.q4_zeros.empty() ? 0 : 1;
+            if (unpack_next) {
+              r.nhwc_out = 1;
+              r.out = Loc{W_OUTPUT, e->ops[i + 1].io_index, 0};
+              unpack_done = true;
+            }
+            const uint64_t bytes = linear_q4_layout(din->c, op.d.cout, op.q4_group, op.q4_scale_dtype, r.q4_zeros != 0, GI_F16).bytes;
+            if (pack) {
+              const uint64_t at = blob_reserve(&e->weight_blob, bytes);
+              linear_q4_pack(LinearQ4Weights{op.q4.data(), op.q4_scales.data(), r.q4_zeros ? op.q4_zeros.data() : nullptr, din->c, op.d.cout,
+                                             op.q4_group, op.q4_scale_dtype, GI_F16},
+                             op.bias.data(), e->weight_blob.data() + at);
+              r.wts = Loc{W_WEIGHTS, 0, at};
+              r.wts_bytes = bytes;
+            }
+          } else if (grouped && pointwise && tc && e->opt.fuse && e->opt.pointwise == GI_PW_AUTO && e->opt.cross_op == GI_XOP_AUTO &&
+                     pointwise_mma_wanted(r)) {
             r.kernel = GI_KERNEL_POINTWISE_MMA;
             r.ep = one_activation(r.ep);
             if (unpack_next) {
@@ -959,7 +986,7 @@ static gi_status lower_pass(const gi_graph& g, gi_exec* e, bool grouped, bool pa
             r.kernel = GI_KERNEL_CONV_SIMT;
             if (pack) pack_conv_simt(op, din->c, e->storage, &e->weight_blob, &r);
           }
-          info.bytes += taps * din->c * op.d.cout * eb;
+          info.bytes += q4 ? op.q4.size() + op.q4_scales.size() + op.q4_zeros.size() : taps * din->c * op.d.cout * eb;
           info.flops = 2 * taps * out_px * din->c * op.d.cout;
         }
         break;

@@ -149,7 +149,7 @@ struct LinearQ4Layout {
 struct LinearQ4Call {
   const void *blob = nullptr, *x = nullptr, *res = nullptr;
   void* y = nullptr;
-  long long x_row = 0, x_slice = 0, y_row = 0, y_slice = 0;
+  long long x_row = 0, x_slice = 0, y_row = 0, y_slice = 0, res_slice = 0;
   int rows = 0, cin = 0, cout = 0, group = 0, scale_dtype = GI_F16, dtype = GI_F16;
   bool zeros = false;
   int plane = 0, real = 0;
@@ -158,6 +158,7 @@ struct LinearQ4Call {
 LinearQ4Layout linear_q4_layout(int cin, int cout, int group, int scale_dtype, bool zeros, int dtype);
 void linear_q4_pack(const LinearQ4Weights& w, const float* bias, uint8_t* blob);  // blob: layout.bytes bytes
 int launch_linear_q4(const LinearQ4Call& c, void* stream);
+int launch_linear_q4_op(const LaunchRec& r, const Ptrs& p, void* stream);  // as an operator of a graph (fp16 storage)
 // the same for many rows, on tcgen05 (linear_q4_tc.cu); reached through it
 bool linear_q4_tc_wanted(const LinearQ4Call& c);
 int launch_linear_q4_tc(const LinearQ4Call& c, const LinearQ4Layout& l, void* stream);

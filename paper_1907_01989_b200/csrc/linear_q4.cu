@@ -51,7 +51,7 @@ struct Params {
   const void* res;
   void* y;
   long long x_row, x_slice;   // elements between rows; between slices of 4 channels (0: channels are contiguous)
-  long long y_row, y_slice;
+  long long y_row, y_slice, res_slice;
   int rows, cin, cout;
   int n_units;                // records along the input channels
   int tiles, kw, ks;          // tiles of output blocks, a cluster of ks CTAs each; parts of a block's sum in a CTA
@@ -166,7 +166,7 @@ __device__ __forceinline__ void store_y(const Params& p, int r, int o, float v) 
     }
     at = row * p.y_row + o;
   }
-  if (p.has_res) v = act_nan(v + __half2float(static_cast<const __half*>(p.res)[(o >> 2) * p.y_slice + r * 4ll + (o & 3)]), p.act_post);
+  if (p.has_res) v = act_nan(v + __half2float(static_cast<const __half*>(p.res)[(o >> 2) * p.res_slice + r * 4ll + (o & 3)]), p.act_post);
   if (XT == GI_F16) static_cast<__half*>(p.y)[at] = __float2half_rn(v);
   else if (XT == GI_BF16) static_cast<__nv_bfloat16*>(p.y)[at] = __float2bfloat16_rn(v);
   else static_cast<float*>(p.y)[at] = v;
@@ -380,7 +380,11 @@ __global__ void __launch_bounds__(kThreads, 2) linear_q4_kernel(const Params p) 
   const int outs = sets * RB * 16, total = outs * nrows;
   for (int i = threadIdx.x + rank * kThreads; i < total; i += kThreads * p.ks) {
     const int r = i / outs, ol = i - r * outs, o = set0 * RB * 16 + ol;
-    if (o >= p.cout) continue;
+    if (o >= p.cout) {
+      // the channels that complete the last slice are zeros
+      if (p.y_slice && o < (p.cout + 3) / 4 * 4) static_cast<__half*>(p.y)[(o >> 2) * p.y_slice + (row0 + r) * 4ll + (o & 3)] = __float2half_rn(0.0f);
+      continue;
+    }
     const int bl = ol >> 4;
     float v = p.bias[o];
     for (int k = 0; k < p.ks; ++k) {
@@ -561,6 +565,31 @@ void linear_q4_pack(const LinearQ4Weights& w, const float* bias, uint8_t* blob) 
   }
 }
 
+int launch_linear_q4_op(const LaunchRec& r, const Ptrs& ptr, void* stream) {
+  LinearQ4Call c;
+  c.blob = ptr.wts;
+  c.x = ptr.in0;
+  c.res = ptr.res;
+  c.y = ptr.out;
+  const int plane = plane_pixels(r.H, r.W);
+  c.rows = r.B * plane;
+  c.cin = r.C;
+  c.cout = r.Co;
+  c.x_slice = c.res_slice = static_cast<long long>(c.rows) * 4;
+  if (r.nhwc_out) {
+    c.y_row = r.Co;
+    c.plane = plane;
+    c.real = r.H * r.W;
+  } else {
+    c.y_slice = c.x_slice;
+  }
+  c.group = r.q4_group;
+  c.scale_dtype = r.q4_scale_dtype;
+  c.zeros = r.q4_zeros != 0;
+  c.ep = r.ep;
+  return launch_linear_q4(c, stream);
+}
+
 int launch_linear_q4(const LinearQ4Call& c, void* stream) {
   if (c.rows <= 0) return 0;
   const LinearQ4Layout l = linear_q4_layout(c.cin, c.cout, c.group, c.scale_dtype, c.zeros, c.dtype);
@@ -579,6 +608,7 @@ int launch_linear_q4(const LinearQ4Call& c, void* stream) {
   p.x_slice = c.x_slice;
   p.y_row = c.y_row;
   p.y_slice = c.y_slice;
+  p.res_slice = c.res_slice;
   p.rows = c.rows;
   p.cin = c.cin;
   p.cout = c.cout;

@@ -10,13 +10,19 @@ from __future__ import annotations
 
 from typing import List, Sequence
 
+from . import api
+
 
 class HostPipeline:
     """Two-slot software pipeline: H2D on a copy stream, gi_run + D2H on the compute stream."""
 
     def __init__(self, ex, input_shapes: Sequence[Sequence[int]], output_shapes: Sequence[Sequence[int]], dtype, device="cuda:0",
-                 slots: int = 2, graphs: bool = False):
-        """graphs: capture each slot's gi_run once as a CUDA graph (its device buffers never change) and replay
+                 slots: int = 2, graphs: bool = False, top: int = 0, temperature: float = 1.0):
+        """top > 0: the executable's one output holds logits [..., classes], and what comes back to the host is not these but their
+        answers (api.log_probs): for each row of logits the log probabilities of its `top` most probable classes, these classes, and
+        the entropy - a few values instead of a row.  submit() then takes host_outputs [rows, top] float32, [rows, top] int32, [rows] float32.
+
+        graphs: capture each slot's gi_run once as a CUDA graph (its device buffers never change) and replay
         it per batch: one launch instead of one per kernel.  Falls back to plain launches if capture fails
         (`self.graphs` then stays empty)."""
         import torch
@@ -27,6 +33,12 @@ class HostPipeline:
         self.copy = torch.cuda.Stream(device)
         self.ins = [[torch.empty(tuple(s), dtype=dtype, device=device) for s in input_shapes] for _ in range(slots)]
         self.outs = [[torch.empty(tuple(s), dtype=dtype, device=device) for s in output_shapes] for _ in range(slots)]
+        self.top, self.temperature, self.answers = top, temperature, []
+        if top:
+            if len(output_shapes) != 1:
+                raise ValueError("answers need an executable with one output, the logits")
+            rows = self.outs[0][0].numel() // output_shapes[0][-1]
+            self.answers = [api.log_probs_out(rows, 0, top, device) for _ in range(slots)]
         self.loaded = [torch.cuda.Event() for _ in range(slots)]   # slot's inputs have arrived
         self.free = [torch.cuda.Event() for _ in range(slots)]     # slot's kernels and read-back are done
         self.used = [False] * slots
@@ -39,18 +51,24 @@ class HostPipeline:
                 caught = []
                 with torch.cuda.stream(side):
                     for s in range(slots):
-                        self.ex.run(self.ins[s], self.outs[s], side)  # warm-up: attributes, tensor maps
+                        self._run(s, side)  # warm-up: attributes, tensor maps
                     side.synchronize()
                     for s in range(slots):
                         cg = torch.cuda.CUDAGraph()
                         with torch.cuda.graph(cg, stream=side):
-                            self.ex.run(self.ins[s], self.outs[s], torch.cuda.current_stream(device))
+                            self._run(s, torch.cuda.current_stream(device))
                         caught.append(cg)
                 self.compute.wait_stream(side)
                 torch.cuda.synchronize(device)
                 self.graphs = caught
             except Exception:  # capture is an optimisation, never a requirement
                 self.graphs = []
+
+    def _run(self, s: int, stream) -> None:
+        self.ex.run(self.ins[s], self.outs[s], stream)
+        if self.top:
+            logits = self.outs[s][0]
+            api.log_probs(logits.view(-1, logits.shape[-1]), top=self.top, temperature=self.temperature, out=self.answers[s], stream=stream)
 
     def submit(self, host_inputs: Sequence, host_outputs: Sequence) -> None:
         """Enqueue one batch: pinned host tensors in, pinned host tensors out.  Asynchronous; results are
@@ -69,8 +87,9 @@ class HostPipeline:
             if self.graphs:
                 self.graphs[s].replay()
             else:
-                self.ex.run(self.ins[s], self.outs[s], self.compute)
-            for h, d in zip(host_outputs, self.outs[s]):
+                self._run(s, self.compute)
+            a = self.answers[s] if self.top else None
+            for h, d in zip(host_outputs, [a.top, a.top_ids, a.entropy] if a else self.outs[s]):
                 h.copy_(d, non_blocking=True)
             self.free[s].record(self.compute)
         self.used[s] = True

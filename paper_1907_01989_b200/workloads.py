@@ -48,6 +48,57 @@ class OpSpec:
     align_corners: bool = True
     weights: Optional[np.ndarray] = None  # fp32, [Cout][kh][kw][Cin]; depthwise [1][kh][kw][C]
     bias: Optional[np.ndarray] = None  # fp32, [Cout]
+    q4: Optional["Q4Weights"] = None  # CONV2D with a 1x1 kernel: the weights in 4 bits (`weights` then holds their values)
+
+
+@dataclass
+class Q4Weights:
+    """Weights of a 1x1 convolution in 4 bits: w[o, k] = scales[o, k / group] * (q[o, k] - zeros[o, k / group])."""
+    q: np.ndarray        # uint8 [Cout][(Cin + 1) / 2], two a byte, the even input channel in the low half
+    scales: np.ndarray   # float16 or float32 [Cout][ceil(Cin / group)]
+    zeros: Optional[np.ndarray]  # uint8, the same shape, 0 .. 15; None: 8 everywhere
+    group: int
+
+    def values(self, cin: int) -> np.ndarray:
+        """The weights themselves, float32 [Cout][1][1][Cin]."""
+        q = np.stack([self.q & 15, self.q >> 4], -1).reshape(self.q.shape[0], -1)[:, :cin].astype(np.float32)
+        of = np.arange(cin) // self.group
+        z = self.zeros.astype(np.float32)[:, of] if self.zeros is not None else np.float32(8)
+        return (self.scales.astype(np.float32)[:, of] * (q - z)).reshape(q.shape[0], 1, 1, cin)
+
+
+def quantize_q4(w: np.ndarray, group: int, zeros: bool = False, scale_dtype=np.float16) -> Q4Weights:
+    """Round float weights [Cout][1][1][Cin] or [Cout][Cin] to 4 bits, group by group: with zero points the range of each group's
+    weights (and 0) on 0 .. 15, without them the largest magnitude on 7 steps either side of 8."""
+    w = np.ascontiguousarray(w, dtype=np.float32).reshape(w.shape[0], -1)
+    cout, cin = w.shape
+    n = -(-cin // group)
+    padded = np.zeros((cout, n * group), dtype=np.float32)
+    padded[:, :cin] = w
+    g = padded.reshape(cout, n, group)
+    if zeros:
+        lo, hi = np.minimum(g.min(2), 0), np.maximum(g.max(2), 0)
+        s = ((hi - lo) / 15).astype(scale_dtype)
+        step = np.where(s > 0, s, 1).astype(np.float32)
+        z = np.clip(np.rint(-lo / step), 0, 15).astype(np.uint8)
+    else:
+        s = (np.abs(g).max(2) / 7).astype(scale_dtype)
+        step = np.where(s > 0, s, 1).astype(np.float32)
+        z = np.full(s.shape, 8, dtype=np.uint8)
+    q = np.clip(np.rint(g / step[..., None]) + z[..., None], 0, 15).astype(np.uint8).reshape(cout, -1)[:, :cin]
+    if cin % 2:
+        q = np.concatenate([q, np.zeros((cout, 1), dtype=np.uint8)], 1)
+    return Q4Weights(np.ascontiguousarray(q[:, 0::2] | (q[:, 1::2] << 4)), s, z if zeros else None, group)
+
+
+def with_q4_classifier(spec: GraphSpec, group: int = 32, zeros: bool = False, scale_dtype=np.float16) -> GraphSpec:
+    """The same network with the weights of its last convolution (1x1) in 4 bits."""
+    op = [o for o in spec.ops if o.kind == CONV2D][-1]
+    if (op.kh, op.kw) != (1, 1):
+        raise ValueError("the last convolution has to be 1x1")
+    op.q4 = quantize_q4(op.weights, group, zeros, scale_dtype)
+    op.weights = op.q4.values(spec.shapes[op.inputs[0]][2])
+    return spec
 
 
 @dataclass
