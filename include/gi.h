@@ -137,7 +137,7 @@ enum {
  * of type weight_dtype (GI_F32 or GI_F16); bias: host pointer to cout floats or NULL.  Both
  * are copied by gi_add_op; the caller may free them as soon as it returns.
  * GI_Q4 (CONV2D with a 1x1 kernel): `weights` points at a gi_q4_weights, whose arrays are copied as well.  A plain 1x1 convolution
- * of few pixels - at most 16 stored ones, as a classifier behind the pooling has - then reads a quarter of the bytes (GI_PW_AUTO,
+ * of few pixels - at most 8 stored ones, as a classifier behind the pooling has at batch 1 to 4 - then reads a quarter of the bytes (GI_PW_AUTO,
  * fp16 storage); everywhere else the weights are expanded by gi_compile, and rounded to fp16 as any others.
  * Unused fields must be zero.  inputs[1] is used by GI_OP_ADD and GI_OP_CONCAT only (elsewhere -1 or 0); there -1
  * means "no second input": the operator is then an identity, which gi_compile removes (Section 3.1).

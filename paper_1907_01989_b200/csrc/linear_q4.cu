@@ -120,7 +120,12 @@ template <int XT>
 __device__ __forceinline__ void stage_x(const Params& p, unsigned char* xs, int pitch, int row0, int nrows, int u0, int n) {
   const int per_row = n * (kUnitK / 8);
   for (int i = threadIdx.x; i < per_row * nrows; i += kThreads) {
-    const int r = i / per_row, c = i - r * per_row, k = u0 * kUnitK + c * 8;
+    int r = i / per_row, c = i - r * per_row;
+    if (p.x_slice) {  // the pixels of a slice are neighbours
+      c = i / nrows;
+      r = i - c * nrows;
+    }
+    const int k = u0 * kUnitK + c * 8;
     if (XT != GI_F32) {
       *reinterpret_cast<uint4*>(xs + r * pitch + c * 16) = load_x8(p, row0 + r, k);
     } else {
@@ -450,16 +455,19 @@ Shape choose_shape(int rows, int cols_per_row, int n_blocks, int n_units, int sm
   s.nt = cols <= 8 ? 1 : cols <= 16 ? 2 : 4;
   s.rb = s.nt == 1 ? 1 : 2;
   const int n_sets = (n_blocks + s.rb - 1) / s.rb;
-  // Two CTAs an SM.  Several rows: pairs of CTAs share x out among themselves, each stages half of its channels (8 rows 4096 -> 12288
-  // 15.1 us, alone 17.0; one row 8192 -> 28672 32.5 and 32.6).  Few outputs of many channels: more CTAs share a sum, as long as each
-  // has 2048 channels of it (4 rows 16384 -> 512: 8 CTAs 7.5 us, 4 7.6, 1 35; one row 1280 -> 1001: 1 CTA 3.0 us, 2 3.5).
-  s.ks = cols >= 4 && n_sets >= sms && n_units >= 2 ? 2 : 1;
+  // Two CTAs an SM.  Several rows: the CTAs of a cluster share x out among themselves, each stages its part of the channels (8 rows
+  // 4096 -> 12288 15.1 us, alone 17.0; 16 rows 4096 -> 4096 12.1, alone 21 - x then takes several rounds of staging; one row 8192 ->
+  // 28672 32.5 and 32.6).  Few outputs of many channels: more CTAs share a sum, as long as each has 2048 channels of it - 512 of
+  // more than 8 columns (4 rows 16384 -> 512: 8 CTAs 7.5 us, 4 7.6, 1 35; 16 rows 2048 -> 2048: 4 6.7, 2 7.9, 1 14.5; one row
+  // 1280 -> 1001: 1 CTA 3.0, 2 3.5).
+  const bool many = cols > 8;
+  s.ks = (many || (cols >= 4 && n_sets >= sms)) && n_units >= 2 ? 2 : 1;
   s.tiles = std::min(n_sets, 2 * sms / s.ks);
-  while (s.ks < 8 && s.tiles * s.ks * 2 <= sms && n_units >= 32 * s.ks) s.ks *= 2;
-  // an item for each warp, of a step or more
+  while (s.ks < 8 && s.tiles * s.ks <= (many ? sms : sms / 2) && n_units >= (many ? 8 : 32) * s.ks) s.ks *= 2;
+  // an item for each warp, or every second one, of a step or more
   s.kw = 1;
   auto sets = [&] { return (n_sets + s.tiles - 1) / s.tiles; };
-  while (s.kw < 8 && sets() * s.kw < kWarps && s.kw * s.ks * 2 <= n_units) s.kw *= 2;
+  while (s.kw < 8 && sets() * s.kw < (many ? kWarps / 2 : kWarps) && s.kw * s.ks * 2 <= n_units) s.kw *= 2;
   const int part = s.rb * cols * 16 * 4;  // bytes of an item's sum
   while (s.kw > 1 && sets() * s.kw * part > kSumBytes) s.kw /= 2;
   if (sets() * part > kSumBytes) {
