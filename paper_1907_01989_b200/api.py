@@ -246,7 +246,7 @@ def _host(t, what: str, dtypes, shape):
 def _rows(t, what: str, dtype, channels: int, device):
     """(pointer, elements between rows, rows) of a device tensor [..., channels] whose leading axes form rows at one pitch."""
     shape = t.shape
-    if t.dtype != dtype or t.device != device or not shape or shape[-1] != channels:
+    if t.dtype is not dtype or t.device != device or not shape or shape[-1] != channels:
         raise ValueError(f"{what}: need {dtype} of shape [..., {channels}] on {device}, got {t.dtype} {tuple(shape)} on {t.device}")
     if len(shape) == 2:
         pitch, step = t.stride()
@@ -345,6 +345,8 @@ def log_probs(logits, given=None, top: int = 0, temperature: float = 1.0, out: O
     import torch
     classes = logits.shape[-1]
     device = logits.device
+    if device.type != "cuda":
+        raise ValueError("logits: need a tensor on a CUDA device")
     ptr, ld, rows = _rows(logits, "logits", logits.dtype, classes, device)
     n_given = 0 if given is None else given.shape[-1]
     if out is None:
@@ -353,7 +355,7 @@ def log_probs(logits, given=None, top: int = 0, temperature: float = 1.0, out: O
     def pointer(t, what, n, dtype):
         if t is None:
             raise ValueError(f"{what}: missing")
-        if t.dtype != dtype or t.device != device or not t.is_contiguous() or t.numel() != rows * n:
+        if t.dtype is not dtype or t.device != device or not t.is_contiguous() or t.numel() != rows * n:
             raise ValueError(f"{what}: need contiguous {dtype} of {rows} x {n} values on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
         return t.data_ptr()
 

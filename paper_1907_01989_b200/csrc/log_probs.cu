@@ -13,7 +13,7 @@
 // ordered bits above the inverted class, so that all are different and no order of execution shows.
 //
 // Three shapes: a thread a row for a handful of classes (every pixel of a segmentation), a warp a row, a CTA a row - or a cluster
-// of up to 16 CTAs, where rows are few: they read one row together and join through distributed shared memory, in a fixed order.
+// of up to 8 CTAs, where rows are few: they read one row together and join through distributed shared memory, in a fixed order.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -321,22 +321,24 @@ __device__ __forceinline__ void write_top(const Params& p, long long row, int j,
 }
 
 // ---------------------------------------------------------------- a CTA, or a cluster of them, for a row
-constexpr int kThreads = 256, kWarps = 8;
-constexpr int kGroups = 64;    // groups of 4 threads, whose largest elements bound the answer
+constexpr int kGroups = 64;    // groups of threads, whose largest elements bound the answer
 constexpr int kFound = 1024;   // elements collected at a time
+constexpr int kMostWarps = 32;
 
 struct Shared {
   alignas(16) u64 group[kGroups];
   u64 found[kFound];
   u64 best[kMaxTop];     // this CTA's answer, largest first; 0: none
-  Stat warp[kWarps], st;
+  Stat warp[kMostWarps], st;
   u64 bound;
   int n_win, n_found;
   int win[kMaxTop];
 };
 
-template <int XT>
-__global__ void __launch_bounds__(kThreads) row_kernel(const Params p) {
+// T: threads of a CTA.
+template <int XT, int T>
+__global__ void __launch_bounds__(T) row_kernel(const Params p) {
+  constexpr int kThreads = T, kWarps = T / 32, kWidth = T / kGroups;
   constexpr int V = Elem<XT>::kVec;
   extern __shared__ __align__(16) unsigned char raw_smem[];
   Shared& sh = *reinterpret_cast<Shared*>(raw_smem);
@@ -364,11 +366,11 @@ __global__ void __launch_bounds__(kThreads) row_kernel(const Params p) {
   }
   if (p.top) {
     u64 g = seen.best(row);
-    g = max64(g, shfl_xor64(g, 1));
-    g = max64(g, shfl_xor64(g, 2));
-    if ((tid & 3) == 0) sh.group[tid >> 2] = g;
+#pragma unroll
+    for (int o = 1; o < kWidth; o <<= 1) g = max64(g, shfl_xor64(g, o));
+    if (tid % kWidth == 0) sh.group[tid / kWidth] = g;
     if (tid == 0) {
-      sh.n_win = 0;
+      sh.n_win = sh.n_found = 0;
       sh.bound = 0;
     }
     if (tid < kMaxTop) sh.best[tid] = 0;
@@ -394,12 +396,10 @@ __global__ void __launch_bounds__(kThreads) row_kernel(const Params p) {
     __syncthreads();
     u64 bound = sh.bound;
     for (;;) {
-      if (tid == 0) sh.n_found = 0;
-      __syncthreads();
       const float bound_v = value_of(bound);
       for (int k = warp; k < sh.n_win; k += kWarps) {
-        // this group's pieces again: lane l takes those of thread l % 4
-        for (int q = rank * kThreads + sh.win[k] * 4 + (lane & 3) + (lane >> 2) * stride; q < row.pieces; q += 8 * stride) {
+        // this group's pieces again, its threads' side by side
+        for (int q = rank * kThreads + sh.win[k] * kWidth + lane % kWidth + lane / kWidth * stride; q < row.pieces; q += 32 / kWidth * stride) {
           const int c0 = q * V - row.lead;
           float v[V];
           Row<XT>::convert(row.piece(q), v);
@@ -428,6 +428,9 @@ __global__ void __launch_bounds__(kThreads) row_kernel(const Params p) {
       // more than fit (large elements at the same places of many pieces): the least of the leading ones found so far bounds the answer
       // more closely, and leaves out all but `top` of what was collected
       bound = sh.best[p.top - 1];
+      __syncthreads();
+      if (tid == 0) sh.n_found = 0;
+      __syncthreads();
     }
   }
   if (p.ks > 1) {
@@ -479,6 +482,7 @@ __global__ void __launch_bounds__(kThreads) row_kernel(const Params p) {
 }
 
 // ---------------------------------------------------------------- a warp for a row
+constexpr int kThreads = 256, kWarps = 8;
 constexpr int kWarpFound = 128;
 
 // N: pieces that a lane requests at a time.
@@ -736,18 +740,18 @@ cudaError_t launch_type(Params& p, cudaStream_t stream) {
     void (*k)(const Params) = p.classes <= 32 * V ? warp_kernel<XT, 1> : p.classes <= 64 * V ? warp_kernel<XT, 2> : warp_kernel<XT, 4>;
     return launch_pdl(k, dim3(grid), dim3(kThreads), 0, stream, static_cast<const Params>(p));
   }
+  // Few rows of many classes: CTAs of 1024 threads, and clusters of CTAs, as long as a thread has three pieces to read (1 x 262144
+  // fp32 9.7 us with 8 CTAs of 1024, 13.4 of 256; 64 x 50257 bf16 9.2 with 2, 10.6 with 8 of 256; 16 x 131072 fp16 8.6 with 4, 16.0
+  // with 8; 1 x 32000 5.2 with 4 of 256, 6.4 with one, 8.5 with 4 of 1024; 2048 x 131072 124 with one of 256, 205 of 1024).
+  const int pieces = p.classes / V;
+  const bool few = p.rows * 2 <= sms && pieces >= 6 * 1024;
+  const int threads = few ? 1024 : 256;
+  void (*k)(const Params) = few ? row_kernel<XT, 1024> : row_kernel<XT, 256>;
   p.ks = 1;
-  while (p.ks < 16 && static_cast<long long>(p.rows) * p.ks < sms && p.classes / V >= 2 * kThreads * p.ks) p.ks *= 2;
-  static bool raised[kMaxDevices] = {};
-  bool& done = raised[current_device_slot()];
-  if (!done) {
-    const cudaError_t err = cudaFuncSetAttribute(row_kernel<XT>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    if (err != cudaSuccess) return err;
-    done = true;
-  }
+  while (p.ks < 8 && static_cast<long long>(p.rows) * p.ks * 2 <= (few ? sms : 2 * sms) && pieces >= 3 * threads * p.ks * 2) p.ks *= 2;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(static_cast<long long>(p.rows) * p.ks));
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = sizeof(Shared);
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
@@ -758,7 +762,7 @@ cudaError_t launch_type(Params& p, cudaStream_t stream) {
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = p.ks > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, row_kernel<XT>, static_cast<const Params>(p));
+  return cudaLaunchKernelEx(&cfg, k, static_cast<const Params>(p));
 }
 
 }  // namespace
