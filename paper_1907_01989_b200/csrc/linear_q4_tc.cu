@@ -127,7 +127,6 @@ __global__ void __launch_bounds__(kThreads, 1) linear_q4_tc_kernel(const __grid_
   const int n_st = 2 * (ub - ua), b_bytes = p.n * kStageK * 2, stage_bytes = kABytes + b_bytes;
   const unsigned full_a = smem_u32(hdr->full_a), full_b = smem_u32(hdr->full_b), empty = smem_u32(hdr->empty), done = smem_u32(&hdr->done);
 
-  pdl_launch_dependents();
   if (threadIdx.x == 0) {
     prefetch_tensormap(&map);
     for (int i = 0; i < p.stages; ++i) {
@@ -145,6 +144,8 @@ __global__ void __launch_bounds__(kThreads, 1) linear_q4_tc_kernel(const __grid_
   }
   __syncthreads();
   tc_fence_after();
+  // only now: a CTA of the next kernel that took this SM's tensor memory first would wait for this kernel's end, and this CTA for it
+  pdl_launch_dependents();
   const unsigned tmem = hdr->tmem;
   int asked = 0;  // copies of x asked for (the copying thread)
 

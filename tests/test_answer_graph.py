@@ -150,3 +150,33 @@ def test_segmentation_to_classes_of_pixels():
     want, bound = ref.log_probs(y.view(-1, y.shape[-1]), None, 1)
     assert torch.equal(got.top_ids.cpu(), want["top_ids"])
     assert ((got.entropy.double().cpu() - want["entropy"]).abs() <= bound["entropy"]).all()
+
+
+@pytest.mark.gpu
+def test_many_rows_between_kernels_that_take_all_tensor_memory():
+    """Each kernel may start while the one in front of it ends: a layer of many rows between 1x1 convolutions on tensor memory, over and
+    over on one stream."""
+    import torch
+    import answer_ref as ref
+    spec = wl.mobilenet_v2(32, size=96)
+    ex = api.graph_from_spec(spec, api.GI_F16)[0].compile(pointwise=api.GI_PW_TC_LANE, cross_op=api.GI_XOP_OFF)
+    assert "pointwise_ts" in [api.KERNEL_NAMES[x.kernel] for x in ex.launches()]
+    ex.bind("cuda:0")
+    x = torch.from_numpy(wl.make_input(spec)).half().cuda()
+    y = torch.empty((32, 1, 1, 1001), dtype=torch.float16, device="cuda:0")
+    q, s, z, b = ref.q4_layer(1, 512, 4096, 64)
+    layer = api.LinearQ4(q, s, z, b, cin=512, group=64)
+    rows = torch.randn((300, 512), generator=torch.Generator().manual_seed(1)).half().cuda()
+    ex.run([x], [y])
+    out = layer.run(rows)
+    torch.cuda.synchronize()
+    first, first_out = y.clone(), out.clone()
+    for _ in range(30):
+        layer.run(rows, out)
+        ex.run([x], [y])
+        layer.run(rows, out)
+        layer.run(rows[:40], out[:40])
+        layer.run(rows, out)
+    torch.cuda.synchronize()
+    assert torch.equal(y, first) and torch.equal(out, first_out)
+    assert api.gi_device_status() == 0
