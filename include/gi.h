@@ -419,7 +419,7 @@ GI_API gi_status gi_linear_q4_blob_bytes(const gi_linear_q4* layer, uint64_t* by
 GI_API gi_status gi_linear_q4_pack(const gi_linear_q4* layer, const uint8_t* q, const void* scales, const uint8_t* zeros, const float* bias,
                                    void* host_blob, uint64_t blob_bytes);
 
-/* Enqueue the product of `rows` >= 0 rows; ldx >= cin, ldy >= cout (not looked at for rows <= 1).  x and y must not overlap. */
+/* Enqueue the product of 0 .. 2^30 rows with the blob that was packed for this very layer; ldx >= cin, ldy >= cout (not looked at for rows <= 1).  x and y must not overlap. */
 GI_API gi_status gi_linear_q4_run(const gi_linear_q4* layer, const void* dev_blob, const void* dev_x, int64_t ldx, void* dev_y, int64_t ldy,
                                   int32_t rows, void* stream);
 

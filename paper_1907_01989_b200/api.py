@@ -272,6 +272,13 @@ def _on(device, stream, call, *args) -> int:
         return call(*args, handle)
 
 
+def _allocating_on(stream):
+    """Tensors made in this context belong to `stream` (a torch Stream): nobody else is given their memory while it still uses it."""
+    import contextlib
+    import torch
+    return torch.cuda.stream(stream) if isinstance(stream, torch.cuda.Stream) else contextlib.nullcontext()
+
+
 class LinearQ4:
     """gi_linear_q4_*: a fully connected layer with 4-bit weights, kept on a device.
 
@@ -308,8 +315,9 @@ class LinearQ4:
         """y[..., cout] = act(x[..., cin] w^T + bias) on `stream` (default: the current one of the layer's device); y is made where none is given.
         Two axes may have any distance between rows; other tensors are contiguous."""
         if y is None:
-            import torch
-            y = torch.empty(tuple(x.shape[:-1]) + (self.cout,), dtype=self.dtype, device=self.device)
+            with _allocating_on(stream):
+                import torch
+                y = torch.empty(tuple(x.shape[:-1]) + (self.cout,), dtype=self.dtype, device=self.device)
         xp, ldx, rows = _rows(x, "x", self.dtype, self.cin, self.device)
         yp, ldy, yrows = _rows(y, "y", self.dtype, self.cout, self.device)
         if rows != yrows:
@@ -350,7 +358,8 @@ def log_probs(logits, given=None, top: int = 0, temperature: float = 1.0, out: O
     ptr, ld, rows = _rows(logits, "logits", logits.dtype, classes, device)
     n_given = 0 if given is None else given.shape[-1]
     if out is None:
-        out = log_probs_out(rows, n_given, top, device)
+        with _allocating_on(stream):
+            out = log_probs_out(rows, n_given, top, device)
 
     def pointer(t, what, n, dtype):
         if t is None:

@@ -73,6 +73,7 @@ gi_status gi_linear_q4_run(const gi_linear_q4* layer, const void* dev_blob, cons
   const gi_status st = check_layer("gi_linear_q4_run", layer);
   if (st != GI_OK) return st;
   if (rows < 0) return fail(GI_E_INVALID, "gi_linear_q4_run: negative number of rows");
+  if (rows > (1 << 30)) return fail(GI_E_UNSUPPORTED, "gi_linear_q4_run: more than 2^30 rows");
   if (rows == 0) return GI_OK;
   if (!dev_blob || !dev_x || !dev_y) return fail(GI_E_INVALID, "gi_linear_q4_run: null argument");
   const int elem = elem_of(layer->dtype);

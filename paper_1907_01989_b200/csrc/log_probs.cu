@@ -483,7 +483,7 @@ __global__ void __launch_bounds__(T) row_kernel(const Params p) {
 
 // ---------------------------------------------------------------- a warp for a row
 constexpr int kThreads = 256, kWarps = 8;
-constexpr int kWarpFound = 128;
+constexpr int kWarpFound = 256;  // (fewer pieces than lanes, all of whose elements may have to be looked at, hold at most 248)
 
 // N: pieces that a lane requests at a time.
 template <int XT, int N>

@@ -128,6 +128,7 @@ def test_refusals_of_run_before_any_launch():
         return L.gi_linear_q4_run(C.byref(d), blob, x, ldx, y, ldy, rows, None)
 
     assert run(rows=0) == api.GI_OK  # no rows: nothing to do
+    assert run(rows=(1 << 30) + 1) == api.GI_E_UNSUPPORTED
     for bad in (dict(rows=-1), dict(blob=None), dict(x=None), dict(y=None), dict(blob=blob + 128), dict(x=x + 1), dict(y=y + 1), dict(ldx=63),
                 dict(ldy=31), dict(ldx=(1 << 30) + 1), dict(y=x), dict(y=x + 64 * 2 * 3), dict(x=y + 32 * 2 * 3)):
         assert run(**bad) == api.GI_E_INVALID, bad
