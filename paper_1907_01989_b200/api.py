@@ -91,7 +91,7 @@ class gi_log_probs_desc(C.Structure):
 EXPORTS = ["gi_graph_create", "gi_graph_input", "gi_add_op", "gi_graph_output", "gi_graph_destroy", "gi_compile",
            "gi_exec_query", "gi_exec_tensor", "gi_exec_op", "gi_exec_launch", "gi_exec_bind", "gi_run", "gi_run_static", "gi_run_timed", "gi_device_status", "gi_selftest_bounded_wait", "gi_exec_destroy",
            "gi_slice8_tensor_bytes", "gi_slice8_pointwise_blob_bytes", "gi_slice8_pointwise_pack", "gi_slice8_pointwise_run",
-           "gi_linear_q4_blob_bytes", "gi_linear_q4_pack", "gi_linear_q4_run", "gi_log_probs",
+           "gi_linear_q4_blob_bytes", "gi_linear_q4_pack", "gi_linear_q4_pack_device", "gi_linear_q4_run", "gi_log_probs",
            "gi_status_str", "gi_last_error", "gi_tensor_bytes", "gi_f32_to_f16"]
 
 _lib = None
@@ -148,6 +148,8 @@ def lib() -> C.CDLL:
     L.gi_linear_q4_blob_bytes.restype = C.c_int32
     L.gi_linear_q4_pack.argtypes = [C.POINTER(gi_linear_q4), vp, vp, vp, vp, vp, C.c_uint64]
     L.gi_linear_q4_pack.restype = C.c_int32
+    L.gi_linear_q4_pack_device.argtypes = [C.POINTER(gi_linear_q4), vp, vp, vp, vp, vp, C.c_uint64, vp]
+    L.gi_linear_q4_pack_device.restype = C.c_int32
     L.gi_linear_q4_run.argtypes = [C.POINTER(gi_linear_q4), vp, vp, C.c_int64, vp, C.c_int64, C.c_int32, vp]
     L.gi_linear_q4_run.restype = C.c_int32
     L.gi_log_probs.argtypes = [C.POINTER(gi_log_probs_desc)] + [vp] * 7
@@ -234,13 +236,13 @@ def _gi_dtype(t) -> int:
     return _GI_DTYPES.get(t.dtype, 0)
 
 
-def _host(t, what: str, dtypes, shape):
-    """`t` (torch tensor on any device, or numpy array) as a contiguous host tensor of one of `dtypes` and of `shape`."""
+def _weights(t, what: str, dtypes, shape):
+    """`t` (torch tensor on any device, or numpy array) as a contiguous tensor, checked to be one of `dtypes` and of `shape`."""
     import torch
     t = torch.from_numpy(np.ascontiguousarray(t)) if isinstance(t, np.ndarray) else t
     if t.dtype not in dtypes or tuple(t.shape) != tuple(shape):
         raise ValueError(f"{what}: need {' or '.join(str(d) for d in dtypes)} of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
-    return t.detach().cpu().contiguous()
+    return t.detach().contiguous()
 
 
 def _rows(t, what: str, dtype, channels: int, device):
@@ -284,26 +286,39 @@ class LinearQ4:
 
     q [cout, (cin + 1) / 2] uint8, two values a byte, the even input channel in the low half; scales [cout, ceil(cin / group)] float16,
     bfloat16 or float32; zeros (optional, else 8 everywhere) uint8 of the scales' shape, 0 .. 15; bias (optional) [cout] float32.
-    Tensors on any device, or numpy arrays; they are copied.  `dtype` is the type of the rows that run() takes and returns.
+    Tensors on any device, or numpy arrays; they are copied: packed on the layer's device where all of them are there (on its current
+    stream), else on the host.  `dtype` is the type of the rows that run() takes and returns.
     """
 
     def __init__(self, q, scales, zeros=None, bias=None, *, cin: int, group: int, dtype: int = GI_F16, act: int = GI_ACT_NONE,
                  device="cuda:0"):
         import torch
         cout, groups = int(q.shape[0]), -(-cin // group) if group > 0 else 0
-        q = _host(q, "q", (torch.uint8,), (cout, (cin + 1) // 2))
-        scales = _host(scales, "scales", (torch.float16, torch.bfloat16, torch.float32), (cout, groups))
-        zeros = None if zeros is None else _host(zeros, "zeros", (torch.uint8,), (cout, groups))
-        bias = None if bias is None else _host(bias, "bias", (torch.float32,), (cout,))
+        q = _weights(q, "q", (torch.uint8,), (cout, (cin + 1) // 2))
+        scales = _weights(scales, "scales", (torch.float16, torch.bfloat16, torch.float32), (cout, groups))
+        zeros = None if zeros is None else _weights(zeros, "zeros", (torch.uint8,), (cout, groups))
+        bias = None if bias is None else _weights(bias, "bias", (torch.float32,), (cout,))
         self.desc = gi_linear_q4(cin, cout, group, _gi_dtype(scales), 0 if zeros is None else 1, dtype, act)
         self._ref = C.byref(self.desc)
         n = C.c_uint64(0)
         _check(lib().gi_linear_q4_blob_bytes(self._ref, C.byref(n)), "gi_linear_q4_blob_bytes")
-        blob = torch.empty(int(n.value), dtype=torch.uint8)
-        _check(lib().gi_linear_q4_pack(self._ref, q.data_ptr(), scales.data_ptr(), None if zeros is None else zeros.data_ptr(),
-                                       None if bias is None else bias.data_ptr(), blob.data_ptr(), blob.numel()), "gi_linear_q4_pack")
+        parts = [t for t in (q, scales, zeros, bias) if t is not None]
+        device = torch.empty(0, device=device).device
+
+        def pointers(ts):
+            return [None if t is None else t.data_ptr() for t in ts]
+        if device.type == "cuda" and all(t.device == device for t in parts):
+            if zeros is not None and bool((zeros > 15).any()):
+                raise ValueError("zeros: 0 .. 15")
+            self.blob = torch.empty(int(n.value), dtype=torch.uint8, device=device)
+            _check(_on(device, None, lib().gi_linear_q4_pack_device, self._ref, *pointers((q, scales, zeros, bias)), self.blob.data_ptr(), self.blob.numel()),
+                   "gi_linear_q4_pack_device")
+        else:
+            host = [None if t is None else t.cpu() for t in (q, scales, zeros, bias)]
+            blob = torch.empty(int(n.value), dtype=torch.uint8)
+            _check(lib().gi_linear_q4_pack(self._ref, *pointers(host), blob.data_ptr(), blob.numel()), "gi_linear_q4_pack")
+            self.blob = blob.to(device)
         self.cin, self.cout, self.dtype = cin, cout, _torch_dtype(dtype)
-        self.blob = blob.to(device)
         self.device = self.blob.device
         self._run = lib().gi_linear_q4_run
 

@@ -68,6 +68,24 @@ gi_status gi_linear_q4_pack(const gi_linear_q4* layer, const uint8_t* q, const v
   return GI_OK;
 }
 
+gi_status gi_linear_q4_pack_device(const gi_linear_q4* layer, const uint8_t* dev_q, const void* dev_scales, const uint8_t* dev_zeros,
+                                   const float* dev_bias, void* dev_blob, uint64_t blob_bytes, void* stream) {
+  const gi_status st = check_layer("gi_linear_q4_pack_device", layer);
+  if (st != GI_OK) return st;
+  if (!dev_q || !dev_scales || !dev_blob) return fail(GI_E_INVALID, "gi_linear_q4_pack_device: null argument");
+  if ((dev_zeros != nullptr) != (layer->has_zeros != 0))
+    return fail(GI_E_INVALID, "gi_linear_q4_pack_device: zeros must be given exactly where has_zeros is 1");
+  if (!aligned_to(dev_blob, 256)) return fail(GI_E_INVALID, "gi_linear_q4_pack_device: the blob must be 256-byte aligned");
+  if (!aligned_to(dev_scales, elem_of(layer->scale_dtype)) || !aligned_to(dev_bias, 4))
+    return fail(GI_E_INVALID, "gi_linear_q4_pack_device: scales or bias not aligned to their elements");
+  if (blob_bytes < linear_q4_layout(layer->cin, layer->cout, layer->group, layer->scale_dtype, dev_zeros != nullptr, layer->dtype).bytes)
+    return fail(GI_E_INVALID, "gi_linear_q4_pack_device: dev_blob too small");
+  const int err = launch_linear_q4_pack(LinearQ4Weights{dev_q, dev_scales, dev_zeros, layer->cin, layer->cout, layer->group, layer->scale_dtype, layer->dtype},
+                                        dev_bias, dev_blob, stream);
+  if (err != 0) return fail(GI_E_CUDA, std::string("gi_linear_q4_pack_device: ") + cudaGetErrorString(static_cast<cudaError_t>(err)));
+  return GI_OK;
+}
+
 gi_status gi_linear_q4_run(const gi_linear_q4* layer, const void* dev_blob, const void* dev_x, int64_t ldx, void* dev_y, int64_t ldy,
                            int32_t rows, void* stream) {
   const gi_status st = check_layer("gi_linear_q4_run", layer);

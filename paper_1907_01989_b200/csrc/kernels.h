@@ -157,6 +157,7 @@ struct LinearQ4Call {
 };
 LinearQ4Layout linear_q4_layout(int cin, int cout, int group, int scale_dtype, bool zeros, int dtype);
 void linear_q4_pack(const LinearQ4Weights& w, const float* bias, uint8_t* blob);  // blob: layout.bytes bytes
+int launch_linear_q4_pack(const LinearQ4Weights& w, const float* bias, void* blob, void* stream);  // everything on the device
 int launch_linear_q4(const LinearQ4Call& c, void* stream);
 int launch_linear_q4_op(const LaunchRec& r, const Ptrs& p, void* stream);  // as an operator of a graph (fp16 storage)
 // the same for many rows, on tcgen05 (linear_q4_tc.cu); reached through it

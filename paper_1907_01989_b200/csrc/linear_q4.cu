@@ -413,6 +413,79 @@ __global__ void __launch_bounds__(kThreads, 2) linear_q4_kernel(const Params p) 
   if (p.ks > 1) cluster_sync();  // nobody leaves while its shared memory is read
 }
 
+// ---------------------------------------------------------------- packing on the device (the host's linear_q4_pack, byte for byte)
+struct PackParams {
+  const unsigned char *q, *scales, *zeros;
+  const float* bias;
+  unsigned char* blob;
+  long long pitch, n_groups;  // bytes of a row of q; groups of a row
+  unsigned long long bias_at, power_at;
+  int cin, cout, group, scale_dtype, n_units, parts, record, zeros_at, wide;
+};
+
+__device__ __forceinline__ float scale_at(const PackParams& p, long long i) {
+  if (p.scale_dtype == GI_F32) return reinterpret_cast<const float*>(p.scales)[i];
+  if (p.scale_dtype == GI_BF16) return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(p.scales)[i]);
+  return __half2float(reinterpret_cast<const __half*>(p.scales)[i]);
+}
+
+// a CTA a record: 64 threads its weights, the others what lies behind them
+__global__ void __launch_bounds__(128) pack_records_kernel(const PackParams p) {
+  const int block = blockIdx.x / p.n_units, u = blockIdx.x % p.n_units, tid = threadIdx.x;
+  unsigned char* rec = p.blob + static_cast<size_t>(blockIdx.x) * p.record;
+  if (tid < 64) {
+    const int i = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+    unsigned word[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const long long at = static_cast<long long>(u) * (kUnitK / 2) + i * 32 + (s >> 1) * 16 + t * 4 + (s & 1) * 2;
+      unsigned v[2][2];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int o = block * 16 + g + 8 * r;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) v[r][k] = o < p.cout && at + k < p.pitch ? p.q[o * p.pitch + at + k] : 0u;
+      }
+      word[s] = (v[0][0] & 15u) | (v[1][0] & 15u) << 4 | (v[0][1] & 15u) << 8 | (v[1][1] & 15u) << 12 | (v[0][0] >> 4) << 16 | (v[1][0] >> 4) << 20 |
+                (v[0][1] >> 4) << 24 | (v[1][1] >> 4) << 28;
+    }
+    *reinterpret_cast<uint4*>(rec + tid * 16) = make_uint4(word[0], word[1], word[2], word[3]);
+    return;
+  }
+  for (int j = tid - 64; j < p.parts * 16; j += 64) {
+    const int h = j >> 4, o = block * 16 + ((j & 15) >> 1) + 8 * (j & 1);
+    const long long at = (static_cast<long long>(u) * kUnitK + h * (kUnitK / p.parts)) / p.group;
+    const long long from = o * p.n_groups + min(at, p.n_groups - 1);
+    const bool real = o < p.cout;
+    if (p.wide) reinterpret_cast<float*>(rec + kUnitWeights)[j] = real ? scale_at(p, from) : 0.0f;
+    else reinterpret_cast<unsigned short*>(rec + kUnitWeights)[j] = real ? reinterpret_cast<const unsigned short*>(p.scales)[from] : static_cast<unsigned short>(0);
+    if (p.zeros) rec[p.zeros_at + j] = real ? p.zeros[from] & 15u : 0u;
+  }
+  for (int j = p.zeros_at + (p.zeros ? p.parts * 16 : 0) + tid - 64; j < p.record; j += 64) rec[j] = 0;
+}
+
+// a warp an output: its bias, and the power of two that brings its largest scale to 1/2 .. 1
+__global__ void __launch_bounds__(128) pack_outputs_kernel(const PackParams p, int outputs) {
+  const int o = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (o >= outputs) return;
+  float largest = 0.0f;
+  for (long long gr = lane; o < p.cout && gr < p.n_groups; gr += 32) {
+    const float v = fabsf(scale_at(p, o * p.n_groups + gr));
+    if (v <= 3.402823466e38f) largest = fmaxf(largest, v);
+  }
+  for (int k = 16; k; k >>= 1) largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, k));
+  if (lane == 0) {
+    float power = 1.0f;
+    if (largest > 0.0f) {
+      int e = 0;
+      frexpf(largest, &e);
+      power = ldexpf(1.0f, min(126, max(-126, -e)));
+    }
+    reinterpret_cast<float*>(p.blob + p.power_at)[o] = power;
+    reinterpret_cast<float*>(p.blob + p.bias_at)[o] = p.bias && o < p.cout ? p.bias[o] : 0.0f;
+  }
+}
+
 template <int XT, int NT, int RB, bool S32>
 cudaError_t launch_shape(const Params& p, int parts, bool zeros, unsigned grid, size_t smem, cudaStream_t stream) {
   void (*k)(const Params) = parts == 1   ? (zeros ? linear_q4_kernel<XT, NT, RB, 1, true, S32> : linear_q4_kernel<XT, NT, RB, 1, false, S32>)
@@ -555,7 +628,8 @@ void linear_q4_pack(const LinearQ4Weights& w, const float* bias, uint8_t* blob) 
       }
       std::memcpy(rec, words, sizeof words);
     }
-  std::memset(blob + l.bias, 0, l.bytes - l.bias);
+  const uint64_t end = static_cast<uint64_t>(l.n_blocks) * l.n_units * l.record;
+  std::memset(blob + end, 0, l.bytes - end);
   if (bias) std::memcpy(blob + l.bias, bias, static_cast<size_t>(w.cout) * sizeof(float));
   // the power of two that brings an output's largest scale to 1/2 .. 1
   for (int o = 0; o < l.n_blocks * 16; ++o) {
@@ -571,6 +645,37 @@ void linear_q4_pack(const LinearQ4Weights& w, const float* bias, uint8_t* blob) 
     }
     std::memcpy(blob + l.power + static_cast<size_t>(o) * 4, &power, 4);
   }
+}
+
+int launch_linear_q4_pack(const LinearQ4Weights& w, const float* bias, void* blob, void* stream) {
+  const LinearQ4Layout l = linear_q4_layout(w.cin, w.cout, w.group, w.scale_dtype, w.zeros != nullptr, w.dtype);
+  PackParams p{};
+  p.q = w.q;
+  p.scales = static_cast<const unsigned char*>(w.scales);
+  p.zeros = w.zeros;
+  p.bias = bias;
+  p.blob = static_cast<unsigned char*>(blob);
+  p.pitch = (static_cast<long long>(w.cin) + 1) / 2;
+  p.n_groups = (static_cast<long long>(w.cin) + w.group - 1) / w.group;
+  p.bias_at = l.bias;
+  p.power_at = l.power;
+  p.cin = w.cin;
+  p.cout = w.cout;
+  p.group = w.group;
+  p.scale_dtype = w.scale_dtype;
+  p.n_units = l.n_units;
+  p.parts = l.parts;
+  p.record = l.record;
+  p.zeros_at = l.zeros_at;
+  p.wide = wide_scales(w.scale_dtype, w.dtype);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const uint64_t end = static_cast<uint64_t>(l.n_blocks) * l.n_units * l.record;
+  const cudaError_t err = cudaMemsetAsync(p.blob + end, 0, l.bytes - end, st);
+  if (err != cudaSuccess) return static_cast<int>(err);
+  const int outputs = l.n_blocks * 16;
+  pack_records_kernel<<<static_cast<unsigned>(l.n_blocks) * l.n_units, 128, 0, st>>>(p);
+  pack_outputs_kernel<<<static_cast<unsigned>(outputs + 3) / 4, 128, 0, st>>>(p, outputs);
+  return static_cast<int>(cudaGetLastError());
 }
 
 int launch_linear_q4_op(const LaunchRec& r, const Ptrs& ptr, void* stream) {

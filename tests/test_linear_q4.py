@@ -136,6 +136,31 @@ def test_refusals_of_run_before_any_launch():
 
 # ---------------------------------------------------------------- GPU
 @pytest.mark.gpu
+@pytest.mark.parametrize("cin,cout,group", [(1, 1, 32), (97, 33, 32), (1280, 1001, 96), (515, 40, 64), (4096, 300, 128), (200, 17, 1 << 30)])
+@pytest.mark.parametrize("scale", [torch.float16, torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("zeros,bias", [(False, True), (True, False)])
+def test_packed_on_the_device_byte_for_byte(cin, cout, group, scale, zeros, bias):
+    for dtype in (torch.float16, torch.bfloat16):
+        q, s, z, b = ref.q4_layer(cin, cin, cout, group, scale, zeros, bias)
+        s[0] = 0
+        if scale == torch.float32:
+            s[cout // 2] *= 2.0 ** 140
+            s[cout - 1] *= 2.0 ** -130
+        kw = dict(cin=cin, group=group, dtype=GI[dtype])
+        host = api.LinearQ4(q, s, z, b, **kw)
+        dev = api.LinearQ4(q.cuda(), s.cuda(), None if z is None else z.cuda(), None if b is None else b.cuda(), **kw)
+        assert dev.blob.device.type == "cuda" and torch.equal(host.blob.cpu(), dev.blob.cpu())
+
+
+@pytest.mark.gpu
+def test_refusals_of_packing_on_the_device():
+    q, s, z, b = (t.cuda() for t in ref.q4_layer(1, 64, 16, 32, zeros=True))
+    z[0, 0] = 16
+    with pytest.raises(ValueError):
+        api.LinearQ4(q, s, z, b, cin=64, group=32)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("rows", [1, 2, 3, 5, 8, 9, 16, 17, 31, 40, 130])
 def test_rows(rows, dtype):
