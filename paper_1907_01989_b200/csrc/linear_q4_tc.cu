@@ -5,7 +5,7 @@
 // channels).  Here a CTA computes 128 outputs x up to 256 rows: the weights are the A operand - sixteen warps, two for each block of 16
 // outputs, expand the records that their own rings of copies bring, scale them and store them to shared memory in the swizzled
 // layout (rows of 64 channels = 128 bytes, 16-byte units exchanged by the row's number) - and the rows of x the B operand, copied by
-// one thread as tiles of the same layout.  One thread issues the products, 128 x N x 16 each; the sums stay in tensor memory until
+// one thread as tiles of the same layout (rows that are not in whole 16-byte units are loaded by the expanding warps instead).  One thread issues the products, 128 x N x 16 each; the sums stay in tensor memory until
 // the last channel.  Expanding a record of 16 x 128 weights is shared by all rows of the tile.  Where outputs are few, the CTAs of a
 // cluster share the input channels and add their sums up through distributed shared memory, in a fixed order.
 //
@@ -45,12 +45,13 @@ constexpr unsigned kErrLoad = 1u, kErrMma = 2u, kErrWork = 4u, kErrDrain = 8u;
 struct Params {
   const unsigned char* wts;
   const float *bias, *power;
+  const unsigned short* x;   // gathered rows only
   void* y;
-  long long y_row;
-  int rows, cout, n_blocks, n_units;
+  long long x_row, y_row;
+  int rows, cin, cout, n_blocks, n_units;
   int m_tiles, n, ks;        // tiles of outputs; rows of a tile; CTAs that share a sum
   int stages, tmem_cols;
-  int act;
+  int act, words;            // words: rows of x in whole 32-bit words
   Masks q;
 };
 
@@ -113,7 +114,23 @@ __device__ __forceinline__ void store_y(const Params& p, int r, int o, float v) 
   else static_cast<__half*>(p.y)[r * p.y_row + o] = __float2half_rn(v);
 }
 
-template <bool BF, int HG, bool ZP, bool S32>
+// Eight channels k .. k + 7 of row r of x, zero behind the last one and behind the last row.
+__device__ __forceinline__ uint4 gather8(const Params& p, int r, int k) {
+  if (r >= p.rows) return make_uint4(0u, 0u, 0u, 0u);
+  const unsigned short* x = p.x + r * p.x_row + k;
+  unsigned v[8];
+  if (p.words) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = k + 2 * i < p.cin ? reinterpret_cast<const unsigned*>(x)[i] : 0u;
+    return make_uint4(v[0], v[1], v[2], v[3]);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = k + i < p.cin ? x[i] : 0u;
+  return make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+}
+
+// GATHER: rows of x that a tiled copy cannot read (not in whole 16-byte units) are loaded by the warps that expand the weights.
+template <bool BF, int HG, bool ZP, bool S32, bool GATHER>
 __global__ void __launch_bounds__(kThreads, 1) linear_q4_tc_kernel(const __grid_constant__ CUtensorMap map, const Params p) {
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   constexpr int kZerosAt = zeros_at(HG, S32), kRecord = record_bytes(HG, S32, ZP), kBehind = kRecord - kUnitWeights;
@@ -128,7 +145,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_q4_tc_kernel(const __grid_
   const unsigned full_a = smem_u32(hdr->full_a), full_b = smem_u32(hdr->full_b), empty = smem_u32(hdr->empty), done = smem_u32(&hdr->done);
 
   if (threadIdx.x == 0) {
-    prefetch_tensormap(&map);
+    if (!GATHER) prefetch_tensormap(&map);
     for (int i = 0; i < p.stages; ++i) {
       mbar_init(full_a + i * 8, kBlocks);
       mbar_init(full_b + i * 8, 1);
@@ -189,6 +206,14 @@ __global__ void __launch_bounds__(kThreads, 1) linear_q4_tc_kernel(const __grid_
       if (u + kRing < ub) request(from);
       copies_commit();
       from = from == ring + (kRing - 1) * kSlot ? ring : from + kSlot;
+      // (the first 32 KB of the rows, half a tile of 256, are asked for ahead of the expansion)
+      const int k0 = u * kUnitK + half * kStageK, chunk = bl * 32 + lane;  // 16-byte units of the tile: 8 a row, 256 by these warps at a time
+      uint4 xv[4];
+      if (GATHER) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (j * 32 < p.n) xv[j] = gather8(p, row0 + j * 32 + chunk / 8, k0 + chunk % 8 * 8);
+      }
       uint4 out[2][2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -216,6 +241,21 @@ __global__ void __launch_bounds__(kThreads, 1) linear_q4_tc_kernel(const __grid_
         sts128(row + at, out[h][0].x, out[h][0].y, out[h][0].z, out[h][0].w);
         sts128(row + 8 * 128 + at, out[h][1].x, out[h][1].y, out[h][1].z, out[h][1].w);
       }
+      if (GATHER) {
+        const unsigned b = st0 + stage * stage_bytes + kABytes;
+        for (int j0 = 0; j0 < p.n; j0 += 128) {
+          if (j0) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (j0 + j * 32 < p.n) xv[j] = gather8(p, row0 + j0 + j * 32 + chunk / 8, k0 + chunk % 8 * 8);
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int r = j0 + j * 32 + chunk / 8;
+            if (r < p.n) sts128(b + r * 128 + static_cast<unsigned>((chunk ^ r) & 7) * 16, xv[j].x, xv[j].y, xv[j].z, xv[j].w);
+          }
+        }
+      }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // visible to the tensor core
       __syncwarp();
       if (lane == 0) mbar_arrive(full_a + stage * 8);
@@ -224,7 +264,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_q4_tc_kernel(const __grid_
     }
     copies_wait<0>();
   } else if (warp == kCopyWarp) {
-    if (lane == 0) {
+    if (!GATHER && lane == 0) {
       pdl_wait();
       int stage = 0, phase = 1;
       for (; asked < n_st; ++asked) {
@@ -240,7 +280,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_q4_tc_kernel(const __grid_
     const unsigned idesc = (1u << 4) | (BF ? (1u << 7) | (1u << 10) : 0u) | (static_cast<unsigned>(p.n >> 3) << 17) | ((kOuts >> 4) << 24);
     int stage = 0, phase = 0;
     for (int it = 0; it < n_st; ++it) {
-      if (!mbar_wait_warp(full_b + stage * 8, phase, abort_flag, kWaitNs, &g_q4_tc_error, kErrMma) ||
+      if ((!GATHER && !mbar_wait_warp(full_b + stage * 8, phase, abort_flag, kWaitNs, &g_q4_tc_error, kErrMma)) ||
           !mbar_wait_warp(full_a + stage * 8, phase, abort_flag, kWaitNs, &g_q4_tc_error, kErrMma))
         break;
       tc_fence_after();
@@ -330,19 +370,22 @@ __global__ void __launch_bounds__(kThreads, 1) linear_q4_tc_kernel(const __grid_
   }
 }
 
-template <bool BF, bool S32>
+template <bool BF, bool S32, bool G>
 void (*kernel_of(int parts, bool zeros))(const CUtensorMap, const Params) {
-  return parts == 1   ? (zeros ? linear_q4_tc_kernel<BF, 1, true, S32> : linear_q4_tc_kernel<BF, 1, false, S32>)
-         : parts == 2 ? (zeros ? linear_q4_tc_kernel<BF, 2, true, S32> : linear_q4_tc_kernel<BF, 2, false, S32>)
-                      : (zeros ? linear_q4_tc_kernel<BF, 4, true, S32> : linear_q4_tc_kernel<BF, 4, false, S32>);
+  return parts == 1   ? (zeros ? linear_q4_tc_kernel<BF, 1, true, S32, G> : linear_q4_tc_kernel<BF, 1, false, S32, G>)
+         : parts == 2 ? (zeros ? linear_q4_tc_kernel<BF, 2, true, S32, G> : linear_q4_tc_kernel<BF, 2, false, S32, G>)
+                      : (zeros ? linear_q4_tc_kernel<BF, 4, true, S32, G> : linear_q4_tc_kernel<BF, 4, false, S32, G>);
+}
+template <bool G>
+void (*kernel_of(bool bf, bool wide, int parts, bool zeros))(const CUtensorMap, const Params) {
+  return bf ? (wide ? kernel_of<true, true, G>(parts, zeros) : kernel_of<true, false, G>(parts, zeros))
+            : (wide ? kernel_of<false, true, G>(parts, zeros) : kernel_of<false, false, G>(parts, zeros));
 }
 
 }  // namespace
 
-// Rows in whole 16-byte units are what a tiled copy can read.
 bool linear_q4_tc_wanted(const LinearQ4Call& c) {
-  return c.rows > 16 && c.dtype != GI_F32 && !c.x_slice && !c.y_slice && !c.plane && !c.ep.has_res &&
-         reinterpret_cast<uintptr_t>(c.x) % 16 == 0 && c.x_row % 8 == 0;
+  return c.rows > 16 && c.dtype != GI_F32 && !c.x_slice && !c.y_slice && !c.plane && !c.ep.has_res;
 }
 
 int launch_linear_q4_tc(const LinearQ4Call& c, const LinearQ4Layout& l, void* stream) {
@@ -353,8 +396,14 @@ int launch_linear_q4_tc(const LinearQ4Call& c, const LinearQ4Layout& l, void* st
   p.power = reinterpret_cast<const float*>(blob + l.power);
   p.y = c.y;
   p.y_row = c.y_row;
+  p.x = static_cast<const unsigned short*>(c.x);
+  p.x_row = c.x_row;
   p.rows = c.rows;
+  p.cin = c.cin;
   p.cout = c.cout;
+  p.words = reinterpret_cast<uintptr_t>(c.x) % 4 == 0 && c.x_row % 2 == 0 && c.cin % 2 == 0;
+  // rows in whole 16-byte units are what a tiled copy can read
+  const bool gather = reinterpret_cast<uintptr_t>(c.x) % 16 != 0 || c.x_row % 8 != 0;
   p.n_blocks = l.n_blocks;
   p.n_units = l.n_units;
   p.act = c.ep.act_pre;
@@ -377,23 +426,22 @@ int launch_linear_q4_tc(const LinearQ4Call& c, const LinearQ4Layout& l, void* st
   const long long grid = p.m_tiles * row_tiles * p.ks;
   if (grid > 0x7fffffffll || p.stages < 2 || smem > static_cast<size_t>(kSmem)) return static_cast<int>(cudaErrorInvalidConfiguration);
 
-  CUtensorMap map;
+  CUtensorMap map{};
   EncodeTiledFn enc = tensor_map_encoder();
-  if (!enc) return static_cast<int>(cudaErrorNotSupported);
+  if (!gather && !enc) return static_cast<int>(cudaErrorNotSupported);
   const cuuint64_t dim[2] = {static_cast<cuuint64_t>(c.cin), static_cast<cuuint64_t>(c.rows)};
   const cuuint64_t pitch[1] = {static_cast<cuuint64_t>(c.x_row) * 2};
   const cuuint32_t box[2] = {kStageK, static_cast<cuuint32_t>(p.n)};
   const cuuint32_t one[2] = {1, 1};
-  if (enc(&map, c.dtype == GI_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(c.x), dim, pitch, box, one,
+  if (!gather && enc(&map, c.dtype == GI_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(c.x), dim, pitch, box, one,
           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return static_cast<int>(cudaErrorInvalidValue);
 
   const int parts = parts_of(c.group);
   const bool wide = wide_scales(c.scale_dtype, c.dtype), bf = c.dtype == GI_BF16;
-  void (*k)(const CUtensorMap, const Params) = bf ? (wide ? kernel_of<true, true>(parts, c.zeros) : kernel_of<true, false>(parts, c.zeros))
-                                                  : (wide ? kernel_of<false, true>(parts, c.zeros) : kernel_of<false, false>(parts, c.zeros));
-  static bool raised[2][2][3][2][kMaxDevices] = {};
-  bool& ready = raised[bf][wide][parts / 2][c.zeros][current_device_slot()];
+  void (*k)(const CUtensorMap, const Params) = gather ? kernel_of<true>(bf, wide, parts, c.zeros) : kernel_of<false>(bf, wide, parts, c.zeros);
+  static bool raised[2][2][2][3][2][kMaxDevices] = {};
+  bool& ready = raised[gather][bf][wide][parts / 2][c.zeros][current_device_slot()];
   if (!ready) {
     const cudaError_t err = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (err != cudaSuccess) return static_cast<int>(err);

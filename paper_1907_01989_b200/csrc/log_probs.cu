@@ -328,10 +328,11 @@ constexpr int kMostWarps = 32;
 struct Shared {
   alignas(16) u64 group[kGroups];
   u64 found[kFound];
+  u64 kept[kMaxTop * (kFound / kGroups)];  // the ones that a second bound leaves of them
   u64 best[kMaxTop];     // this CTA's answer, largest first; 0: none
   Stat warp[kMostWarps], st;
   u64 bound;
-  int n_win, n_found;
+  int n_win, n_found, n_kept;
   int win[kMaxTop];
 };
 
@@ -415,12 +416,36 @@ __global__ void __launch_bounds__(T) row_kernel(const Params p) {
         }
       }
       __syncthreads();
-      const int found = sh.n_found, n = min(found, kFound);
+      const int found = sh.n_found;
+      int n = min(found, kFound);
+      const u64* list = sh.found;
+      if (n > 2 * kGroups) {
+        // many (equal ones, as in a row of which nothing is left): the same bound once more, from 64 shares of what was found
+        if (tid < kGroups) {
+          u64 m = 0;
+          for (int k = tid; k < n; k += kGroups) m = max64(m, sh.found[k]);
+          sh.group[tid] = m;
+        }
+        if (tid == 0) sh.n_kept = 0;
+        __syncthreads();
+        if (tid < kGroups) {
+          const u64 mine = sh.group[tid];
+          int above = 0;
+          for (int k = 0; k < kGroups; ++k) above += sh.group[k] > mine;
+          if (above == p.top - 1) sh.bound = mine;
+        }
+        __syncthreads();
+        for (int k = tid; k < n; k += kThreads)
+          if (sh.found[k] >= sh.bound) sh.kept[atomicAdd(&sh.n_kept, 1)] = sh.found[k];
+        __syncthreads();
+        n = sh.n_kept;
+        list = sh.kept;
+      }
       // their order: an element's place is the number of larger ones
       for (int k = tid; k < n; k += kThreads) {
-        const u64 mine = sh.found[k];
+        const u64 mine = list[k];
         int above = 0;
-        for (int j = 0; j < n; ++j) above += sh.found[j] > mine;
+        for (int j = 0; j < n; ++j) above += list[j] > mine;
         if (above < p.top) sh.best[above] = mine;
       }
       __syncthreads();

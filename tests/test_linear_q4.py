@@ -189,9 +189,11 @@ def test_groups_scales_and_zero_points(group, scale, zeros):
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
 @pytest.mark.parametrize("rows", [17, 32, 33, 64, 100, 128, 250, 256, 257, 300, 513, 1000])
-def test_many_rows(rows, dtype):
-    layer, w = make(rows, 1096, 300, 32, dtype, zeros=True)
-    check(rows_of(rows, rows, 1096, dtype), layer, w, 32)
+@pytest.mark.parametrize("cin", [1096, 1097, 1098])
+def test_many_rows(rows, dtype, cin):
+    """Rows in whole 16-byte units, in single elements, in 32-bit words."""
+    layer, w = make(rows, cin, 300, 32, dtype, zeros=True)
+    check(rows_of(rows, rows, cin, dtype), layer, w, 32)
 
 
 @pytest.mark.gpu

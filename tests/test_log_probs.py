@@ -138,6 +138,20 @@ def test_masks(classes, dtype, rows):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,classes", [(3, 50257), (64, 60000), (400, 50257), (5, 1999), (2, 262144)])
+@pytest.mark.parametrize("top", [1, 8, 32])
+def test_rows_of_equal_logits(rows, classes, top):
+    """Nothing left, one value everywhere, two values: every element reaches the bound, the lower classes come first."""
+    x = torch.zeros((rows, classes), dtype=torch.bfloat16)
+    x[0] = -INF
+    x[1] = 3.0
+    x[1, classes // 3::7] = 4.0
+    if rows > 2:
+        x[2, ::2] = -INF
+    check(x, None, top)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
 @pytest.mark.parametrize("rows,classes", [(8, 21), (5000, 21), (8, 1001), (8, 20000)])
 def test_not_a_number_and_infinity_stay_in_their_row(dtype, rows, classes):
