@@ -12,6 +12,10 @@
 // Rounding: scale * (q - zero) is rounded once to x's type here (q - zero alone would need a sum of its own for each group: as many
 // reads of tensor memory as products).  A power of two for each output, which brings its largest scale to 1/2 .. 1, keeps the products
 // inside fp16 whatever the scales are; the sum is multiplied by its inverse.  Scales in 32 bits enter as two parts.
+//
+// Measured (B200): 256 rows 4096 -> 12288 34.5 us (0.75 PFLOP/s on 96 of the 148 SMs), 1024 rows 100 us (1.03), 32 rows 24.5 us - bound
+// by the expansion: some 200 instructions for 16 x 64 weights - and 256 rows 4096 -> 4096 18 us with 4 CTAs to a sum.  Stores of
+// two rows to the same banks took 38 instead of 34.5 us, eight expanding warps instead of sixteen 42.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
