@@ -259,6 +259,15 @@ def _rows(t, what: str, dtype, channels: int, device):
     raise ValueError(f"{what}: channels must be contiguous, and all of a tensor of other than two axes (strides {t.stride()})")
 
 
+def _values(t, what: str, n: int, dtype, device) -> int:
+    """Pointer of a contiguous device tensor of n values."""
+    if t is None:
+        raise ValueError(f"{what}: missing")
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{what}: need {n} contiguous values of {dtype} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
 def _on(device, stream, call, *args) -> int:
     """call(*args, stream handle) with `device` current: the library launches on the current device."""
     import torch
@@ -376,21 +385,14 @@ def log_probs(logits, given=None, top: int = 0, temperature: float = 1.0, out: O
         with _allocating_on(stream):
             out = log_probs_out(rows, n_given, top, device)
 
-    def pointer(t, what, n, dtype):
-        if t is None:
-            raise ValueError(f"{what}: missing")
-        if t.dtype is not dtype or t.device != device or not t.is_contiguous() or t.numel() != rows * n:
-            raise ValueError(f"{what}: need contiguous {dtype} of {rows} x {n} values on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
-        return t.data_ptr()
-
     f32, i32 = torch.float32, torch.int32
     gp = op = ep = ip = tp = None
     if n_given:
-        gp, op = pointer(given, "given", n_given, i32), pointer(out.given, "out.given", n_given, f32)
+        gp, op = _values(given, "given", rows * n_given, i32, device), _values(out.given, "out.given", rows * n_given, f32, device)
     if out.entropy is not None:
-        ep = pointer(out.entropy, "out.entropy", 1, f32)
+        ep = _values(out.entropy, "out.entropy", rows, f32, device)
     if top:
-        ip, tp = pointer(out.top_ids, "out.top_ids", top, i32), pointer(out.top, "out.top", top, f32)
+        ip, tp = _values(out.top_ids, "out.top_ids", rows * top, i32, device), _values(out.top, "out.top", rows * top, f32, device)
     d = gi_log_probs_desc(rows, classes, ld, _gi_dtype(logits), temperature, n_given, top)
     status = _on(device, stream, lib().gi_log_probs, C.byref(d), ptr, gp, op, ep, ip, tp)
     if status != GI_OK:

@@ -15,7 +15,7 @@
 // Measured (B200): 2048 x 131072 fp16 124 us (4.3 TB/s), without `top` 105 us (5.1); 4.2 M rows of 21 classes 87 us (3.0); 1 x 262144
 // fp32 9.7 us, 1 x 1001 5 us.
 //
-// Three shapes: a thread a row for a handful of classes (every pixel of a segmentation), a warp a row, a CTA a row - or a cluster
+// Three shapes: a thread a row for a handful of classes (every pixel of a segmentation), a warp a row (few classes, or many rows), a CTA a row - or a cluster
 // of up to 8 CTAs, where rows are few: they read one row together and join through distributed shared memory, in a fixed order.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -552,10 +552,16 @@ __global__ void __launch_bounds__(kThreads) warp_kernel(const Params p) {
   int n = 0;
   const unsigned before = (1u << lane) - 1u;
   for (int i = lane; __any_sync(0xffffffffu, i < row.pieces); i += 32) {
-    float v[V];
     const int c0 = i * V - row.lead;
-    const bool look = i < row.pieces && seen.most >= bound;
-    if (look) Row<XT>::convert(row.piece(i), v);
+    bool look = i < row.pieces && seen.most >= bound;
+    uint4 w = make_uint4(0u, 0u, 0u, 0u);
+    if (look) {
+      w = row.piece(i);
+      look = ordered(Elem<XT>::most(w)) >= bound;
+    }
+    if (!__any_sync(0xffffffffu, look)) continue;  // (most pieces)
+    float v[V];
+    Row<XT>::convert(w, v);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       const bool hit = look && ordered(v[j]) >= bound && c0 + j >= 0 && c0 + j < row.classes;
@@ -755,7 +761,9 @@ cudaError_t launch_type(Params& p, cudaStream_t stream) {
     }
     return launch_pdl(k, dim3(grid), dim3(kThreadRows), smem, stream, static_cast<const Params>(p));
   }
-  if (p.classes <= 2048) {
+  // A warp a row: few classes, or enough rows to fill the GPU with warps (fp16, top 5: 5000 x 5000 31 us, with a CTA a row 46; 50000 x
+  // 3000 151 and 458; but 1200 x 5000 19 and 14, 20000 x 10000 fp32 385 and 281).
+  if (p.classes <= 2048 || (p.classes / V <= 1024 && p.rows >= 16 * sms)) {
     const unsigned grid = static_cast<unsigned>((static_cast<long long>(p.rows) + kWarps - 1) / kWarps);
     void (*k)(const Params) = p.classes <= 32 * V ? warp_kernel<XT, 1> : p.classes <= 64 * V ? warp_kernel<XT, 2> : warp_kernel<XT, 4>;
     return launch_pdl(k, dim3(grid), dim3(kThreads), 0, stream, static_cast<const Params>(p));

@@ -83,7 +83,7 @@ def test_many_rows_of_few_classes(classes, dtype, pitch):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("rows,classes", [(1, 1001), (300, 1001), (700, 5000), (2000, 2500), (148, 40000), (3, 200000)])
+@pytest.mark.parametrize("rows,classes", [(1, 1001), (300, 1001), (700, 5000), (2000, 2500), (148, 40000), (3, 200000), (2400, 5003), (2400, 8192)])
 def test_rows(rows, classes):
     x = logits_of(rows, rows, classes, torch.float16)
     check(x, torch.zeros((rows, 1), dtype=torch.int32), 5)
