@@ -99,6 +99,29 @@ def test_graph_matches_the_oracle(batch, H, W, cin, cout, kw, planner):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("zeros", [False, True])
+def test_fp32_storage_and_the_built_in_arena(zeros):
+    import torch
+    import gpu_util as gu
+    from oracle import graph as og
+    spec = q4_graph(2, 1, 1, 130, 45, zeros=zeros, relu=wl.ACT_RELU6, follow=True)
+    x = np.random.default_rng(3).uniform(-1, 1, (2, 1, 1, 130)).astype(np.float16).astype(np.float32)
+    got = gu.DeviceRun(spec, storage=api.GI_F32).run([x])
+    gu.assert_close(got[spec.outputs[0]], og.run(spec, [x], storage="f32")[spec.outputs[0]], api.GI_F32)
+    ex = api.graph_from_spec(spec, api.GI_F16)[0].compile()
+    ex.bind("cuda:0")
+    assert "linear_q4" in [api.KERNEL_NAMES[k.kernel] for k in ex.launches()]
+    xin = torch.from_numpy(x).half().cuda()
+    a, b = (torch.full((2, 1, 1, 24), float("nan"), dtype=torch.float16, device="cuda") for _ in range(2))
+    ex.run([xin], [a])
+    ex.arena.fill_(0xFF)
+    ex.run_static([xin], [b])
+    torch.cuda.synchronize()
+    assert torch.equal(a, b) and torch.isfinite(a).all()
+    assert len(ex.run_timed([xin], [b])) == ex.info.n_ops
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("batch", [1, 4, 8, 12])
 @pytest.mark.parametrize("graphs", [False, True])
 def test_network_to_answers(batch, graphs):

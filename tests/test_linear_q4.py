@@ -354,3 +354,20 @@ def test_a_blob_written_just_before_the_call_is_the_one_used():
         y1 = a.run(x)
         a.blob.bitwise_xor_(flip)
         assert torch.equal(y0, ya) and torch.equal(y1, yb), i
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,pitch,dtype", [(3, 1 << 30, torch.float16), (20, (1 << 27) + 8, torch.bfloat16), (20, (1 << 27) + 3, torch.float16), (2, 1 << 30, torch.float32)])
+def test_rows_far_beyond_32_bits(rows, pitch, dtype):
+    """Row offsets of more than 2^32 bytes, in x and in y."""
+    layer, w = make(1, 192, 40, 64, dtype)
+    x = rows_of(2, rows, 192, dtype)
+    wide = torch.as_strided(torch.empty((rows - 1) * pitch + 192, dtype=dtype, device="cuda"), (rows, 192), (pitch, 1))
+    wide.copy_(x)
+    check_near = ref.linear_q4(x, *w, 64)
+    got = layer.run(wide)
+    assert ((got.double().cpu() - check_near[0]).abs() <= check_near[1]).all()
+    del wide
+    far = torch.as_strided(torch.empty((rows - 1) * pitch + 40, dtype=dtype, device="cuda"), (rows, 40), (pitch, 1))
+    layer.run(x.cuda(), far)
+    assert torch.equal(far, layer.run(x.cuda()))

@@ -207,6 +207,15 @@ def test_rows_far_beyond_32_bits():
 
 
 @pytest.mark.gpu
+def test_many_rows_far_beyond_32_bits():
+    rows, classes, pitch = 4100, 21, (1 << 20) + 5
+    dev = torch.as_strided(torch.empty((rows - 1) * pitch + classes, dtype=torch.float16, device="cuda"), (rows, classes), (pitch, 1))
+    x = logits_of(4, rows, classes, torch.float16)
+    dev.copy_(x)
+    check(x, None, 3, dev=dev)
+
+
+@pytest.mark.gpu
 def test_only_what_is_asked_for():
     x = logits_of(5, 12, 1001, torch.float16)
     got = check(x)
