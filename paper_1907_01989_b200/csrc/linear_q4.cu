@@ -9,8 +9,8 @@
 // fp32 for each group of input channels and are scaled in fp32: nothing of a weight is rounded.  For so few columns tcgen05 would
 // only add a store to shared memory for every weight; from 17 rows on it wins (linear_q4_tc.cu).
 //
-// Measured (B200): one row 8192 -> 28672 32 us, 3.7 TB/s (its copies alone 23 us, its arithmetic alone 27), one row 4096 -> 4096
-// 5.4 us, 8 rows 4096 -> 12288 14 us, 16 rows 5120 -> 13824 28.5 us.
+// Measured (B200): one row 8192 -> 28672 31.4 us, 3.9 TB/s (its copies alone 23 us, its arithmetic alone 27), one row 4096 -> 4096
+// 5.9 us, 8 rows 4096 -> 12288 13 us, 16 rows 5120 -> 13824 23 us.
 //
 // x in 32 bits: a value is the exact sum of three bf16 numbers (8 + 8 + 8 digits), so a row of x becomes three columns of the product.
 //
@@ -40,11 +40,13 @@ using namespace ptx;
 using namespace frag;
 using namespace q4;
 
-// A warp's ring of copies: slots of two records (neighbours of one block, or one of each of two blocks).  Two CTAs of 8 warps keep
-// 128 KB of an SM's requests open.
+// One CTA an SM: two of 8 warps would each stage x (8 rows 4096 -> 12288 13.0 us, two CTAs 15.2; 16 rows 8192 -> 8192 22.8 and 27.3;
+// one row 8192 -> 28672 31.4 and 33.1, 4096 -> 4096 5.9 and 5.5).
+constexpr int kWarps = 16, kThreads = kWarps * 32;
+// A warp's ring of copies: slots of two records (neighbours of one block, or one of each of two blocks).  16 warps keep 128 KB of
+// requests open.
 constexpr int kSlots = 4;
-// most shared memory of a CTA: two CTAs of 8 warps on an SM, or one of 16
-constexpr int kSmemTwo = 113 * 1024, kSmemOne = 226 * 1024;
+constexpr int kSmem = 226 * 1024;         // one CTA on an SM
 constexpr int kSumBytes = 16384;          // most for the items' sums: with the rings (records of up to 1344 bytes) and one step of x inside that
 
 struct Params {
@@ -119,7 +121,7 @@ __device__ __forceinline__ void split3(float v, unsigned (&s)[3]) {
 }
 
 // Rows of x for units [u0, u0 + n) into shared memory, `pitch` bytes a row.
-template <int XT, int kThreads>
+template <int XT>
 __device__ __forceinline__ void stage_x(const Params& p, unsigned char* xs, int pitch, int row0, int nrows, int u0, int n) {
   const int per_row = n * (kUnitK / 8);
   for (int i = threadIdx.x; i < per_row * nrows; i += kThreads) {
@@ -180,14 +182,10 @@ __device__ __forceinline__ void store_y(const Params& p, int r, int o, float v) 
   else static_cast<float*>(p.y)[at] = v;
 }
 
-// warps of a CTA: with more than 8 columns x takes the room of a second CTA
-__host__ __device__ constexpr int warps_of(int nt) { return nt == 1 ? 8 : 16; }
-
 // XT: type of x and y.  NT: eights of columns (rows of x, three for a row of 32 bits).  RB: blocks of 16 outputs of a warp.
 // HG: groups that a record may touch, 1, 2 or 4 parts of it.  ZP: zero points of the groups (else 8 everywhere).  S32: scales in 32 bits.
 template <int XT, int NT, int RB, int HG, bool ZP, bool S32>
-__global__ void __launch_bounds__(warps_of(NT) * 32, NT == 1 ? 2 : 1) linear_q4_kernel(const Params p) {
-  constexpr int kWarps = warps_of(NT), kThreads = kWarps * 32;
+__global__ void __launch_bounds__(kThreads, 1) linear_q4_kernel(const Params p) {
   extern __shared__ __align__(128) unsigned char smem[];
   constexpr bool BF = XT != GI_F16;
   constexpr int kCols = XT == GI_F32 ? 3 : 1;  // columns of a row of x
@@ -332,7 +330,7 @@ __global__ void __launch_bounds__(warps_of(NT) * 32, NT == 1 ? 2 : 1) linear_q4_
   unsigned from = ring;
   for (int c = 0; c < chunks; ++c) {
     if (c) __syncthreads();  // every warp is done with the chunk before
-    stage_x<XT, kThreads>(p, smem, pitch, row0, nrows, ua + c * p.chunk, min(p.chunk, ub - ua - c * p.chunk));
+    stage_x<XT>(p, smem, pitch, row0, nrows, ua + c * p.chunk, min(p.chunk, ub - ua - c * p.chunk));
     __syncthreads();
     for (int item = warp; item < items; item += kWarps) {
       int first, last;
@@ -501,13 +499,13 @@ cudaError_t launch_shape(const Params& p, int parts, bool zeros, unsigned grid, 
   static bool raised[3][2][kMaxDevices] = {};
   bool& done = raised[parts / 2][zeros][current_device_slot()];
   if (!done) {
-    const cudaError_t err = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, NT == 1 ? kSmemTwo : kSmemOne);
+    const cudaError_t err = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (err != cudaSuccess) return err;
     done = true;
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(warps_of(NT) * 32);
+  cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
@@ -535,20 +533,19 @@ Shape choose_shape(int rows, int cols_per_row, int n_blocks, int n_units, int sm
   s.nt = cols <= 8 ? 1 : cols <= 16 ? 2 : 4;
   s.rb = s.nt == 1 ? 1 : 2;
   const int n_sets = (n_blocks + s.rb - 1) / s.rb;
-  // Up to 8 columns two CTAs an SM, above that one of 16 warps, whose x is staged once (16 rows 8192 -> 8192 22.8 us, two CTAs of 8
-  // warps 27.3).  Several rows: the CTAs of a cluster share x out among themselves, each stages its part of the channels (8 rows 4096
-  // -> 12288 15.1 us, alone 17.0; 16 rows 8192 -> 8192 22.8 and 28.5; one row 8192 -> 28672 32.5 and 32.6).  Few outputs of many
-  // channels: more CTAs share a sum, as long as each has 2048 channels of it - 512 of more than 8 columns (4 rows 16384 -> 512: 8
-  // CTAs 7.5 us, 4 7.6, 1 35; 12 rows 1280 -> 1001: 2 4.5, 4 5.6; one row 1280 -> 1001: 1 CTA 3.0, 2 3.5).
+  // More than 8 columns: pairs of CTAs share x out among themselves, each stages half of its channels (16 rows 8192 -> 8192 22.8 us,
+  // alone 28.5; 8 rows 4096 -> 12288 13.0 and 12.9).  Few outputs of many channels: more CTAs share a sum, as long as each has 2048
+  // channels of it - 512 of more than 8 columns (4 rows 16384 -> 512: 8 CTAs 7.5 us, 4 7.6, 1 35; 12 rows 1280 -> 1001: 2 4.5, 4 5.6;
+  // one row 1280 -> 1001: 1 CTA 2.9, 2 3.5).
   const bool many = cols > 8;
-  const int slots = many ? sms : 2 * sms;
-  s.ks = (many || (cols >= 4 && n_sets >= sms)) && n_units >= 2 ? 2 : 1;
-  s.tiles = std::min(n_sets, slots / s.ks);
+  s.ks = many && n_units >= 2 ? 2 : 1;
+  s.tiles = std::min(n_sets, sms / s.ks);
   while (s.ks < 8 && s.tiles * s.ks * 2 <= sms && n_units >= (many ? 8 : 32) * s.ks) s.ks *= 2;
-  // items: one for each of 8 warps, of a step or more (16 rows 4096 -> 4096, 2 sets of outputs a CTA: 4 parts 9.8 us, 2 10.1, 1 12.7)
+  // items for most of the warps, of a step or more (16 rows 4096 -> 4096, 2 sets of outputs a CTA: 4 parts 9.8 us, 2 10.1, 1 12.7;
+  // one row 8192 -> 28672, 12 sets: 4 31.2, 2 31.4, 1 32.2)
   s.kw = 1;
   auto sets = [&] { return (n_sets + s.tiles - 1) / s.tiles; };
-  while (s.kw < (many ? 4 : 8) && sets() * s.kw < 8 && s.kw * s.ks * 2 <= n_units) s.kw *= 2;
+  while (s.kw < (many ? 4 : 8) && sets() * s.kw < (many ? 8 : 14) && s.kw * s.ks * 2 <= n_units) s.kw *= 2;
   const int part = s.rb * cols * 16 * 4;  // bytes of an item's sum
   while (s.kw > 1 && sets() * s.kw * part > kSumBytes) s.kw /= 2;
   if (sets() * part > kSumBytes) {
@@ -740,11 +737,10 @@ int launch_linear_q4(const LinearQ4Call& c, void* stream) {
   const int elem = c.dtype == GI_F32 ? 4 : 2, cols = s.row_tile * cols_per_row;
   p.tiles = s.tiles;
   p.x_vec = c.x_slice == 0 && reinterpret_cast<uintptr_t>(c.x) % 16 == 0 && (c.rows == 1 || c.x_row * elem % 16 == 0);
-  // shared memory: x (as much of it as two CTAs on an SM leave room for), the rings of copies, the items' sums
+  // shared memory: x (as much of it as there is room for), the rings of copies, the items' sums
   const int n_sets = (l.n_blocks + s.rb - 1) / s.rb, sets = (n_sets + s.tiles - 1) / s.tiles;
-  const int most = s.nt == 1 ? kSmemTwo : kSmemOne;
-  const int rings = warps_of(s.nt) * kSlots * 2 * l.record, sums = sets * s.kw * s.rb * cols * 16 * 4;
-  const int fit = ((most - rings - sums) / cols - 64) / (kUnitK * 2);
+  const int rings = kWarps * kSlots * 2 * l.record, sums = sets * s.kw * s.rb * cols * 16 * 4;
+  const int fit = ((kSmem - rings - sums) / cols - 64) / (kUnitK * 2);
   const int need = (l.n_units + s.ks - 1) / s.ks, step = 2 / s.rb;
   p.chunk = std::max(1, std::min(fit / step, (need + step - 1) / step)) * step;
   p.ring_at = (cols * (p.chunk * kUnitK * 2 + 64) + 127) / 128 * 128;
@@ -756,7 +752,7 @@ int launch_linear_q4(const LinearQ4Call& c, void* stream) {
   p.real = c.real;
   const size_t smem = static_cast<size_t>(p.red_at) + sums;
   const long long grid = static_cast<long long>(p.tiles) * s.ks * ((c.rows + s.row_tile - 1) / s.row_tile);
-  if (grid > 0x7fffffffll || smem > static_cast<size_t>(most)) return static_cast<int>(cudaErrorInvalidConfiguration);
+  if (grid > 0x7fffffffll || smem > static_cast<size_t>(kSmem)) return static_cast<int>(cudaErrorInvalidConfiguration);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const unsigned n = static_cast<unsigned>(grid);
   const int parts = parts_of(c.group);
