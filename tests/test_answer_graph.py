@@ -203,3 +203,41 @@ def test_many_rows_between_kernels_that_take_all_tensor_memory():
     torch.cuda.synchronize()
     assert torch.equal(y, first) and torch.equal(out, first_out)
     assert api.gi_device_status() == 0
+
+
+@pytest.mark.gpu
+def test_captured_behind_work_of_two_streams():
+    """A capture in which both operators follow kernels of another stream as well."""
+    import torch
+    import answer_ref as ref
+    q, s, z, b = ref.q4_layer(1, 256, 1001, 64)
+    layer = api.LinearQ4(q, s, z, b, cin=256, group=64)
+    a, c = (torch.randn((30, 256), generator=torch.Generator().manual_seed(i)).half().cuda() for i in (1, 2))
+    x, y = torch.empty_like(a), torch.empty((30, 1001), dtype=torch.float16, device="cuda")
+    out = api.log_probs_out(30, 0, 4)
+    want_y = layer.run(a + c)
+    want = api.log_probs(want_y, top=4)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        main = torch.cuda.current_stream()
+        side.wait_stream(main)
+        with torch.cuda.stream(side):
+            t = a * 1
+        u = c * 1
+        main.wait_stream(side)
+        torch.add(t, u, out=x)
+        layer.run(x, y)
+        side.wait_stream(main)
+        with torch.cuda.stream(side):
+            e = y * 1
+        layer.run(x, y)
+        main.wait_stream(side)
+        api.log_probs(y, top=4, out=out)
+    for _ in range(3):
+        x.zero_()
+        y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want_y) and torch.equal(e, want_y)
+        assert all(torch.equal(p, r) for p, r in zip(out[1:], want[1:]))
