@@ -102,10 +102,11 @@ struct Elem<GI_F32> {
   }
 };
 
-// a value's bits as a whole number of the same order; a NaN above all, -0 as 0
+// A value's bits as a whole number of the same order; a NaN above all values, -0 as 0.  (One NaN's bits stand for all: with a class
+// beside them they are still below the whole numbers that a search for the next smaller key starts from.)
 __device__ __forceinline__ int ordered(float v) {
   int b = __float_as_int(v + 0.0f);
-  if (v != v) b = 0x7fffffff;
+  if (v != v) b = 0x7fc00000;
   return b ^ ((b >> 31) & 0x7fffffff);
 }
 // that above the inverted class: larger values first, then lower classes

@@ -1,6 +1,7 @@
 """Log probabilities of classes, entropy and leading classes: gi_log_probs against a plain form in 64 bits."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
@@ -279,3 +280,31 @@ def test_same_bits_every_time_on_streams_and_in_graphs(rows, classes):
     for o in out:
         assert all(torch.equal(a, b) for a, b in zip(o[1:], again[1:]))
     assert not torch.equal(again.top_ids, want.top_ids)
+
+
+def order_of(x, top):
+    """The leading classes: a NaN above all, of equals the lower class."""
+    v = x.double().numpy()
+    v = np.where(np.isnan(v), np.inf, np.where(np.isposinf(v), np.finfo(np.float64).max, v))
+    return torch.from_numpy(np.lexsort((np.broadcast_to(np.arange(x.shape[1]), x.shape), -v), axis=1)[:, :top].copy()).int()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,classes", [(4096 + 130, 2), (4096 + 130, 8), (4096 + 130, 21), (4096 + 130, 33), (4096 + 130, 64),  # a thread a row
+                                          (12, 8), (12, 21), (12, 1001),  # a warp a row
+                                          (12, 5001), (12, 60000)])  # a CTA a row, a cluster
+def test_not_a_number_leads_from_every_class(dtype, rows, classes):
+    x = logits_of(classes, rows, classes, dtype)
+    places = [[0], [classes // 2], [classes - 1], [0, classes - 1], list(range(classes)), [0, 1]]
+    with_nan = [i * 2 for i in range(len(places))] + [rows - 1]  # the last row too: nothing lies behind it
+    for r, cols in zip(with_nan, places + [[0]]):
+        x[r, cols] = float("nan")
+    x[1, classes - 1] = INF  # below a NaN, above all others
+    x[2, 0] = INF
+    for top in {2, 3, min(classes, 32)} - ({3} if classes < 3 else set()):
+        got = api.log_probs(x.cuda(), None, top)
+        torch.cuda.synchronize()
+        assert torch.equal(got.top_ids.cpu(), order_of(x, top)), top
+        assert torch.isnan(got.top[with_nan]).all() and torch.isnan(got.entropy[with_nan]).all()
+        assert torch.isfinite(got.top[3:10:2]).all()
