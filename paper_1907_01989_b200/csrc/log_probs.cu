@@ -757,8 +757,16 @@ cudaError_t launch_type(Params& p, cudaStream_t stream) {
                               : p.classes <= 40 ? thread_kernel<XT, 25, 40>
                                                 : thread_kernel<XT, 41, kFew>;
     if (smem > 48 * 1024) {
-      const cudaError_t err = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
-      if (err != cudaSuccess) return err;
+      // (only the kernel of the most classes comes here.  Its limit is raised once, to the most that any call needs: other threads' calls
+      // of other sizes may lie between this line and the launch.)
+      static bool raised[kMaxDevices] = {};
+      bool& done = raised[current_device_slot()];
+      if (!done) {
+        const cudaError_t err = cudaFuncSetAttribute(thread_kernel<XT, 41, kFew>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                     static_cast<int>(2 * (kThreadRows * kFew + 2 * V) * sizeof(typename Elem<XT>::type)));
+        if (err != cudaSuccess) return err;
+        done = true;
+      }
     }
     return launch_pdl(k, dim3(grid), dim3(kThreadRows), smem, stream, static_cast<const Params>(p));
   }

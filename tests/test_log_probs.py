@@ -308,3 +308,31 @@ def test_not_a_number_leads_from_every_class(dtype, rows, classes):
         assert torch.equal(got.top_ids.cpu(), order_of(x, top)), top
         assert torch.isnan(got.top[with_nan]).all() and torch.isnan(got.entropy[with_nan]).all()
         assert torch.isfinite(got.top[3:10:2]).all()
+
+
+@pytest.mark.gpu
+def test_calls_of_several_threads_at_once():
+    """Sizes that share a kernel but not their need of shared memory, from threads of their own: none is refused, none is wrong."""
+    import ctypes as C
+    import threading
+    run = api.lib().gi_log_probs
+    results, cases = [], []
+    for classes in (48, 64, 50, 63):
+        x = logits_of(classes, 4096, classes, torch.float32).cuda()
+        want, out, stream = api.log_probs(x, None, 1), api.log_probs_out(4096, 0, 1), torch.cuda.Stream()
+        d = api.gi_log_probs_desc(4096, classes, classes, api.GI_F32, 1.0, 0, 1)
+        cases.append((d, x, want, out, stream))
+    torch.cuda.synchronize()
+
+    def calls(d, x, want, out, stream):
+        args = (C.byref(d), x.data_ptr(), None, None, out.entropy.data_ptr(), out.top_ids.data_ptr(), out.top.data_ptr(), stream.cuda_stream)
+        results.append(sum(run(*args) != api.GI_OK for _ in range(20000)))
+    threads = [threading.Thread(target=calls, args=c) for c in cases]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert results == [0] * len(cases)
+    for _, _, want, out, _ in cases:
+        assert all(torch.equal(a, b) for a, b in zip(out[1:], want[1:]))
