@@ -170,7 +170,11 @@ __device__ __forceinline__ Stat warp_merge(Stat st, float c, int width) {
 
 // log p of a logit, given a row's sums: minus infinity in a row in which nothing is left
 __device__ __forceinline__ float log_prob(float v, const Stat& st, float log_s, float inv_t) {
-  return st.s == 0.0f ? -INFINITY : (v - st.m) * inv_t - log_s;
+  if (st.s == 0.0f) return -INFINITY;
+  float d = (v - st.m) * inv_t;
+  // two numbers whose difference is none in fp32: halves of them, which the temperature may bring back into its range
+  if (d == -INFINITY) d = 2.0f * ((0.5f * v - 0.5f * st.m) * inv_t);
+  return d - log_s;
 }
 __device__ __forceinline__ float entropy_of(const Stat& st, float log_s) { return st.s == 0.0f ? 0.0f : log_s - st.t * kLn2 / st.s; }
 

@@ -336,3 +336,18 @@ def test_calls_of_several_threads_at_once():
     assert results == [0] * len(cases)
     for _, _, want, out, _ in cases:
         assert all(torch.equal(a, b) for a, b in zip(out[1:], want[1:]))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,classes", [(4100, 21), (9, 1001), (3, 70000)])
+def test_logits_whose_difference_is_beyond_fp32(dtype, rows, classes):
+    """The largest and the lowest logit are 6e38 apart: divided by a temperature that is a number again."""
+    x = torch.full((rows, classes), -3e38).to(dtype)
+    x[:, 3], x[:, 5], x[1, 7] = 3e38, 1e38, -INF
+    given = torch.tensor([[0, 5, 7, 3]], dtype=torch.int32).repeat(rows, 1)
+    for temperature in (3.0, 1000.0):
+        got = check(x, given, 4, temperature)
+        assert torch.isfinite(got.top).all()
+    got = api.log_probs(x.cuda(), given.cuda(), 4, 1.0)  # here it is not
+    assert (got.given[:, 0] == -INF).all() and (got.given[:, 3] == 0).all()
