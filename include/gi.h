@@ -424,7 +424,8 @@ GI_API gi_status gi_linear_q4_pack(const gi_linear_q4* layer, const uint8_t* q, 
 GI_API gi_status gi_linear_q4_pack_device(const gi_linear_q4* layer, const uint8_t* dev_q, const void* dev_scales, const uint8_t* dev_zeros,
                                           const float* dev_bias, void* dev_blob, uint64_t blob_bytes, void* stream);
 
-/* Enqueue the product of 0 .. 2^30 rows with the blob that was packed for this very layer; ldx >= cin, ldy >= cout (not looked at for rows <= 1).  x and y must not overlap. */
+/* Enqueue the product of 0 .. 2^30 rows with the blob that was packed for this very layer; ldx >= cin, ldy >= cout (not looked at for rows <= 1).  x and y must not
+ * overlap; their rows may lie between one another, as columns of one tensor, where ldx == ldy. */
 GI_API gi_status gi_linear_q4_run(const gi_linear_q4* layer, const void* dev_blob, const void* dev_x, int64_t ldx, void* dev_y, int64_t ldy,
                                   int32_t rows, void* stream);
 

@@ -29,12 +29,16 @@ gi_status check_layer(const char* who, const gi_linear_q4* l) {
   return GI_OK;
 }
 
-// bytes from the first to behind the last element of a tensor of rows
-uint64_t extent(int64_t rows, int64_t ld, int64_t n, int elem) { return (static_cast<uint64_t>(rows - 1) * ld + n) * elem; }
-
-bool overlap(const void* a, uint64_t na, const void* b, uint64_t nb) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + nb && y < x + na;
+// Whether an element of x is one of y: [rows][cin] and [rows][cout], rows ldx and ldy elements apart.  Rows at one and the same distance
+// may lie between one another (columns of one tensor); of rows at other distances the whole ranges count.
+bool overlap(const void* x, int64_t ldx, int64_t cin, const void* y, int64_t ldy, int64_t cout, int64_t rows, int elem) {
+  const uint64_t a = reinterpret_cast<uintptr_t>(x), b = reinterpret_cast<uintptr_t>(y);
+  const uint64_t na = (static_cast<uint64_t>(rows - 1) * ldx + cin) * elem, nb = (static_cast<uint64_t>(rows - 1) * ldy + cout) * elem;
+  if (a >= b + nb || b >= a + na) return false;
+  if (ldx != ldy) return true;
+  const uint64_t pitch = static_cast<uint64_t>(ldx) * elem;
+  const uint64_t behind = b >= a ? (b - a) % pitch : (pitch - (a - b) % pitch) % pitch;  // y's row behind the start of a row of x
+  return behind < static_cast<uint64_t>(cin) * elem || behind + static_cast<uint64_t>(cout) * elem > pitch;
 }
 
 constexpr int64_t kMaxPitch = int64_t{1} << 30;  // elements between rows: with 2^31 rows and 4 bytes, below 2^63 bytes
@@ -103,7 +107,7 @@ gi_status gi_linear_q4_run(const gi_linear_q4* layer, const void* dev_blob, cons
   }
   if (ldx < layer->cin || ldy < layer->cout) return fail(GI_E_INVALID, "gi_linear_q4_run: rows overlap (ldx < cin or ldy < cout)");
   if (ldx > kMaxPitch || ldy > kMaxPitch) return fail(GI_E_INVALID, "gi_linear_q4_run: ldx or ldy too large");
-  if (overlap(dev_x, extent(rows, ldx, layer->cin, elem), dev_y, extent(rows, ldy, layer->cout, elem)))
+  if (overlap(dev_x, ldx, layer->cin, dev_y, ldy, layer->cout, rows, elem))
     return fail(GI_E_INVALID, "gi_linear_q4_run: x and y overlap");
   LinearQ4Call c;
   c.blob = dev_blob;

@@ -371,3 +371,26 @@ def test_rows_far_beyond_32_bits(rows, pitch, dtype):
     far = torch.as_strided(torch.empty((rows - 1) * pitch + 40, dtype=dtype, device="cuda"), (rows, 40), (pitch, 1))
     layer.run(x.cuda(), far)
     assert torch.equal(far, layer.run(x.cuda()))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [3, 16, 40])
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+def test_x_and_y_side_by_side_in_one_buffer(rows, dtype):
+    """Columns of one tensor: the rows of x and y lie between one another, no element is in both."""
+    cin, cout = 200, 77
+    layer, w = make(9, cin, cout, 64, dtype)
+    x = rows_of(3, rows, cin, dtype)
+    want, bound = ref.linear_q4(x, *w, 64)
+    for x_at, y_at in ((0, cin), (cout, 0), (3, cin + 5), (cout + 5, 2)):
+        pitch = max(x_at + cin, y_at + cout) + 1
+        both = torch.full((rows, pitch), 5.0, dtype=dtype, device="cuda")
+        both[:, x_at:x_at + cin] = x.cuda()
+        y = layer.run(both[:, x_at:x_at + cin], both[:, y_at:y_at + cout])
+        assert ((y.double().cpu() - want).abs() <= bound).all()
+        assert torch.equal(both[:, x_at:x_at + cin].cpu(), x)
+        for at in (cin - 1, -(cout - 1)):  # one column in both
+            at += x_at
+            if 0 <= at and at + cout <= pitch:
+                with pytest.raises(api.GiError):
+                    layer.run(both[:, x_at:x_at + cin], both[:, at:at + cout])
