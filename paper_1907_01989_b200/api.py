@@ -283,11 +283,17 @@ def _on(device, stream, call, *args) -> int:
         return call(*args, handle)
 
 
-def _allocating_on(stream):
-    """Tensors made in this context belong to `stream` (a torch Stream): nobody else is given their memory while it still uses it."""
+def _allocating_on(stream, device):
+    """Tensors made in this context belong to `stream` (a torch Stream, or the handle of one): nobody else is given their memory while
+    it still uses it."""
     import contextlib
     import torch
-    return torch.cuda.stream(stream) if isinstance(stream, torch.cuda.Stream) else contextlib.nullcontext()
+    if stream is None:
+        return contextlib.nullcontext()
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = _stream_ptr(stream)
+        stream = torch.cuda.ExternalStream(handle, device) if handle else torch.cuda.default_stream(device)
+    return torch.cuda.stream(stream)
 
 
 class LinearQ4:
@@ -339,8 +345,8 @@ class LinearQ4:
         """y[..., cout] = act(x[..., cin] w^T + bias) on `stream` (default: the current one of the layer's device); y is made where none is given.
         Two axes may have any distance between rows; other tensors are contiguous."""
         if y is None:
-            with _allocating_on(stream):
-                import torch
+            import torch
+            with _allocating_on(stream, self.device):
                 y = torch.empty(tuple(x.shape[:-1]) + (self.cout,), dtype=self.dtype, device=self.device)
         xp, ldx, rows = _rows(x, "x", self.dtype, self.cin, self.device)
         yp, ldy, yrows = _rows(y, "y", self.dtype, self.cout, self.device)
@@ -382,7 +388,7 @@ def log_probs(logits, given=None, top: int = 0, temperature: float = 1.0, out: O
     ptr, ld, rows = _rows(logits, "logits", logits.dtype, classes, device)
     n_given = 0 if given is None else given.shape[-1]
     if out is None:
-        with _allocating_on(stream):
+        with _allocating_on(stream, device):
             out = log_probs_out(rows, n_given, top, device)
 
     f32, i32 = torch.float32, torch.int32

@@ -394,3 +394,28 @@ def test_x_and_y_side_by_side_in_one_buffer(rows, dtype):
             if 0 <= at and at + cout <= pitch:
                 with pytest.raises(api.GiError):
                     layer.run(both[:, x_at:x_at + cin], both[:, at:at + cout])
+
+
+@pytest.mark.gpu
+def test_results_belong_to_the_stream_whose_handle_was_given():
+    """Memory of a result that is dropped goes to no other stream: its own may still be writing it."""
+    layer, _ = make(6, 256, 4096, 32, torch.float16)
+    x = torch.zeros((512, 256), dtype=torch.float16, device="cuda")
+    side = torch.cuda.Stream()
+    for stream in (side, side.cuda_stream):
+        torch.cuda.synchronize()
+        y = layer.run(x, stream=stream)
+        at = y.data_ptr()
+        del y
+        assert torch.empty((512, 4096), dtype=torch.float16, device="cuda").data_ptr() != at
+        torch.cuda.synchronize()
+        logits = torch.zeros((300000, 2), dtype=torch.float16, device="cuda")
+        torch.cuda.synchronize()
+        got = api.log_probs(logits, stream=stream)
+        at = got.entropy.data_ptr()
+        del got
+        assert torch.empty((300000,), device="cuda").data_ptr() != at
+    torch.cuda.synchronize()
+    y = layer.run(x, stream=0)  # the default stream by its handle
+    torch.cuda.synchronize()
+    assert torch.equal(y, layer.run(x))
