@@ -379,7 +379,7 @@ def log_probs_out(rows: int, n_given: int = 0, top: int = 0, device="cuda:0", en
 def log_probs(logits, given=None, top: int = 0, temperature: float = 1.0, out: Optional[LogProbs] = None, stream=None) -> LogProbs:
     """gi_log_probs: logits [..., classes] (float16, bfloat16, float32; two axes may have any distance between rows, other tensors are
     contiguous) -> log probabilities of `given` (int32 [..., n], negative: nothing asked), entropy and the `top` leading classes of
-    each row, in `out` (log_probs_out) or in new tensors."""
+    each row, in `out` (log_probs_out; what is not asked for is left as it is there, and None in the result) or in new tensors."""
     import torch
     classes = logits.shape[-1]
     device = logits.device
@@ -403,6 +403,8 @@ def log_probs(logits, given=None, top: int = 0, temperature: float = 1.0, out: O
     status = _on(device, stream, lib().gi_log_probs, C.byref(d), ptr, gp, op, ep, ip, tp)
     if status != GI_OK:
         _check(status, "gi_log_probs")
+    if (not n_given and out.given is not None) or (not top and (out.top is not None or out.top_ids is not None)):
+        out = out._replace(given=out.given if n_given else None, top=out.top if top else None, top_ids=out.top_ids if top else None)
     return out
 
 

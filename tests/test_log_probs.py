@@ -339,6 +339,20 @@ def test_calls_of_several_threads_at_once():
 
 
 @pytest.mark.gpu
+def test_buffers_for_more_than_is_asked_for():
+    """What was not asked for is None, not what an earlier call left in its buffer."""
+    x = logits_of(5, 12, 1001, torch.float16).cuda()
+    given = torch.zeros((12, 2), dtype=torch.int32, device="cuda")
+    out = api.log_probs_out(12, 2, 4)
+    full = api.log_probs(x, given, 4, out=out)
+    assert all(a is b for a, b in zip(full, out))
+    got = api.log_probs(x, None, 4, out=out)
+    assert got.given is None and got.top is out.top and got.top_ids is out.top_ids and got.entropy is out.entropy
+    got = api.log_probs(x, given, out=out)
+    assert got.given is out.given and got.top is None and got.top_ids is None
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("rows,classes", [(4100, 21), (9, 1001), (3, 70000)])
 def test_logits_whose_difference_is_beyond_fp32(dtype, rows, classes):
