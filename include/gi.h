@@ -397,9 +397,11 @@ GI_API gi_status gi_slice8_pointwise_run(const void* dev_in, void* dev_out, cons
 /* Fully connected layer with 4-bit weights:
  *   y[r,o] = act(bias[o] + sum_k w[o,k] x[r,k]),   w[o,k] = scale[o, k / group] * (q[o,k] - zero[o, k / group])
  * with q and zero whole numbers of 0 .. 15.  Up to 16 rows, and for GI_F32, nothing of a weight is rounded: q - zero is exact, sums are
- * fp32 for each group before its scale is applied, and y is rounded once (GI_F32: x counts with all its 24 digits, down to 2^-110).
- * For more rows of a 16-bit type each weight may be rounded once to that type, as the weights of a convolution are.  What an infinity
- * or a NaN in a row of x leads to stays in that row of y.
+ * fp32 for each group before its scale is applied (so the sums of (q - zero) x have to be numbers of fp32), and y is rounded once
+ * (GI_F32: x counts with all its 24 digits, down to 2^-110).  For more rows of a 16-bit type a weight enters as the sum of two numbers of
+ * that type: exactly where scale_dtype is a 16-bit type, else within 2^-14 (GI_BF16) or 2^-20 (GI_F16) of itself; for GI_F16 within
+ * 2^-31 of its output's largest scale on top of that.  Sums are fp32.  What an infinity or a NaN in a row of x leads to stays in that row
+ * of y.
  * (Section 3.2 treats the 1x1 convolution as an operator of its own; the paper has no counterpart of the weights' type.) */
 typedef struct gi_linear_q4 {
   int32_t cin, cout;      /* up to 2^20 each */

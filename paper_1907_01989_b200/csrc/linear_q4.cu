@@ -425,7 +425,7 @@ struct PackParams {
   unsigned char* blob;
   long long pitch, n_groups;  // bytes of a row of q; groups of a row
   unsigned long long bias_at, power_at;
-  int cin, cout, group, scale_dtype, n_units, parts, record, zeros_at, wide;
+  int cin, cout, group, scale_dtype, n_units, parts, record, zeros_at, wide, top;
 };
 
 __device__ __forceinline__ float scale_at(const PackParams& p, long long i) {
@@ -469,7 +469,7 @@ __global__ void __launch_bounds__(128) pack_records_kernel(const PackParams p) {
   for (int j = p.zeros_at + (p.zeros ? p.parts * 16 : 0) + tid - 64; j < p.record; j += 64) rec[j] = 0;
 }
 
-// a warp an output: its bias, and the power of two that brings its largest scale to 1/2 .. 1
+// a warp an output: its bias, and the power of two that brings its largest scale to 2^(top - 1) .. 2^top
 __global__ void __launch_bounds__(128) pack_outputs_kernel(const PackParams p, int outputs) {
   const int o = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (o >= outputs) return;
@@ -484,7 +484,7 @@ __global__ void __launch_bounds__(128) pack_outputs_kernel(const PackParams p, i
     if (largest > 0.0f) {
       int e = 0;
       frexpf(largest, &e);
-      power = ldexpf(1.0f, min(126, max(-126, -e)));
+      power = ldexpf(1.0f, min(126, max(-126, p.top - e)));
     }
     reinterpret_cast<float*>(p.blob + p.power_at)[o] = power;
     reinterpret_cast<float*>(p.blob + p.bias_at)[o] = p.bias && o < p.cout ? p.bias[o] : 0.0f;
@@ -636,7 +636,7 @@ void linear_q4_pack(const LinearQ4Weights& w, const float* bias, uint8_t* blob) 
   const uint64_t end = static_cast<uint64_t>(l.n_blocks) * l.n_units * l.record;
   std::memset(blob + end, 0, l.bytes - end);
   if (bias) std::memcpy(blob + l.bias, bias, static_cast<size_t>(w.cout) * sizeof(float));
-  // the power of two that brings an output's largest scale to 1/2 .. 1
+  // the power of two that brings an output's largest scale to 2^(top - 1) .. 2^top
   for (int o = 0; o < l.n_blocks * 16; ++o) {
     float largest = 0.0f, power = 1.0f;
     for (int64_t gr = 0; o < w.cout && gr < n_groups; ++gr) {
@@ -646,7 +646,7 @@ void linear_q4_pack(const LinearQ4Weights& w, const float* bias, uint8_t* blob) 
     if (largest > 0.0f) {
       int e = 0;
       std::frexp(largest, &e);
-      power = std::ldexp(1.0f, std::min(126, std::max(-126, -e)));
+      power = std::ldexp(1.0f, std::min(126, std::max(-126, power_top(w.dtype) - e)));
     }
     std::memcpy(blob + l.power + static_cast<size_t>(o) * 4, &power, 4);
   }
@@ -673,6 +673,7 @@ int launch_linear_q4_pack(const LinearQ4Weights& w, const float* bias, void* blo
   p.record = l.record;
   p.zeros_at = l.zeros_at;
   p.wide = wide_scales(w.scale_dtype, w.dtype);
+  p.top = power_top(w.dtype);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const uint64_t end = static_cast<uint64_t>(l.n_blocks) * l.n_units * l.record;
   const cudaError_t err = cudaMemsetAsync(p.blob + end, 0, l.bytes - end, st);

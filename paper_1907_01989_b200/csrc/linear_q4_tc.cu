@@ -9,13 +9,16 @@
 // the last channel.  Expanding a record of 16 x 128 weights is shared by all rows of the tile.  Where outputs are few, the CTAs of a
 // cluster share the input channels and add their sums up through distributed shared memory, in a fixed order.
 //
-// Rounding: scale * (q - zero) is rounded once to x's type here (q - zero alone would need a sum of its own for each group: as many
-// reads of tensor memory as products).  A power of two for each output, which brings its largest scale to 1/2 .. 1, keeps the products
-// inside fp16 whatever the scales are; the sum is multiplied by its inverse.  Scales in 32 bits enter as two parts.
+// Precision: scale * (q - zero) enters as the sum of two numbers of x's type, the nearest one and what that leaves, each with a product and
+// a sum of its own (where the first sum is no number, the second does not count: what is left may be 0 or of the other sign).  For scales
+// in 16 bits (times 4 bits of q - zero) the two are all of it; of a scale in 32 bits, which enters in two parts as well, 16 digits or more
+// are left in bf16, 22 in fp16.  fp16 lacks range: a power of two for each output brings its largest scale to 2^11 .. 2^12, where 15 times
+// it is still a number; what lies below the smallest step there is 2^-31 of that scale at most.  Weights rounded once would take 24.7
+// instead of 31.4 us for 32 rows and 35 instead of 51 for 256.  q - zero alone, exact, needs sums of its own for each group, which
+// the sixteen warps have to read out of tensor memory, scale and add up: 35 us for 32 rows, 78 for 256, with groups of 32 50 and 113.
 //
-// Measured (B200): 256 rows 4096 -> 12288 34.5 us (0.75 PFLOP/s on 96 of the 148 SMs), 1024 rows 100 us (1.03), 32 rows 24.5 us - bound
-// by the expansion: some 200 instructions for 16 x 64 weights - and 256 rows 4096 -> 4096 18 us with 4 CTAs to a sum.  Stores of
-// two rows to the same banks took 38 instead of 34.5 us, eight expanding warps instead of sixteen 42.
+// Measured (B200, 4096 -> 12288): 256 rows 51 us, 1024 rows 147 - two products for each weight, 1.0 and 1.4 PFLOP/s of them, the
+// former on 96 of the 148 SMs - 32 rows 31.4 us, bound by the expansion, and 256 rows 4096 -> 4096 23 us with 4 CTAs to a sum.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -40,7 +43,7 @@ constexpr int kCopyWarp = kWorkers, kMmaWarp = kWorkers + 1;
 constexpr int kThreads = (kWorkers + 2) * 32;
 constexpr int kOuts = 128, kStageK = 64;       // outputs of a CTA, channels of a stage
 constexpr int kABytes = kOuts * kStageK * 2;
-constexpr int kMaxStages = 4, kRing = 4;       // records that a worker has in flight
+constexpr int kMaxStages = 4, kRing = 3;       // records that a worker has in flight
 constexpr int kHeader = 1024;
 constexpr unsigned kWaitNs = 1000000000u;
 constexpr int kSmem = 227 * 1024;
@@ -111,6 +114,17 @@ __device__ __forceinline__ unsigned fma(unsigned a, unsigned b, unsigned c) {
   return *reinterpret_cast<const unsigned*>(&r);
 }
 
+// a b - c
+template <bool BF>
+__device__ __forceinline__ unsigned fms(unsigned a, unsigned b, unsigned c) {
+  if (BF) {
+    const __nv_bfloat162 r = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b), __hneg2(*reinterpret_cast<const __nv_bfloat162*>(&c)));
+    return *reinterpret_cast<const unsigned*>(&r);
+  }
+  const __half2 r = __hfma2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b), __hneg2(*reinterpret_cast<const __half2*>(&c)));
+  return *reinterpret_cast<const unsigned*>(&r);
+}
+
 template <bool BF>
 __device__ __forceinline__ void store_y(const Params& p, int r, int o, float v) {
   v = act_nan(v, p.act);
@@ -145,7 +159,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_q4_tc_kernel(const __grid_
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = blockIdx.x % p.ks, mt = blockIdx.x / p.ks % p.m_tiles, row0 = blockIdx.x / p.ks / p.m_tiles * p.n;
   const int ua = static_cast<int>(static_cast<long long>(p.n_units) * rank / p.ks), ub = static_cast<int>(static_cast<long long>(p.n_units) * (rank + 1) / p.ks);
-  const int n_st = 2 * (ub - ua), b_bytes = p.n * kStageK * 2, stage_bytes = kABytes + b_bytes;
+  const int n_st = 2 * (ub - ua), b_bytes = p.n * kStageK * 2, stage_bytes = 2 * kABytes + b_bytes;  // (a stage: weights, what they leave, rows)
   const unsigned full_a = smem_u32(hdr->full_a), full_b = smem_u32(hdr->full_b), empty = smem_u32(hdr->empty), done = smem_u32(&hdr->done);
 
   if (threadIdx.x == 0) {
@@ -218,11 +232,11 @@ __global__ void __launch_bounds__(kThreads, 1) linear_q4_tc_kernel(const __grid_
         for (int j = 0; j < 4; ++j)
           if (j * 32 < p.n) xv[j] = gather8(p, row0 + j * 32 + chunk / 8, k0 + chunk % 8 * 8);
       }
-      uint4 out[2][2];
+      uint4 out[2][2][2];  // the weights; what they leave
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const Zero z = ZP ? zero_of<BF>(p.q, zp[h] & 255u, zp[h] >> 8) : zero_of<BF>(p.q, 8u, 8u);
-        unsigned s0, s1, r0, r1, a[2][4];
+        unsigned s0, s1, r0, r1, a[2][4], left[2][4];
         halves<BF>(f[h].x * power_lo, s0, r0);
         halves<BF>(f[h].y * power_hi, s1, r1);
 #pragma unroll
@@ -230,23 +244,30 @@ __global__ void __launch_bounds__(kThreads, 1) linear_q4_tc_kernel(const __grid_
           expand<BF>(p.q, word[2 * h + s], z, a[s]);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const unsigned sc = e & 1 ? s1 : s0, rest = e & 1 ? r1 : r0;
-            a[s][e] = S32 ? fma<BF>(a[s][e], sc, mul<BF>(a[s][e], rest)) : mul<BF>(a[s][e], sc);
+            const unsigned v = a[s][e], sc = e & 1 ? s1 : s0, rest = e & 1 ? r1 : r0;
+            a[s][e] = S32 ? fma<BF>(v, sc, mul<BF>(v, rest)) : mul<BF>(v, sc);
+            left[s][e] = fms<BF>(v, sc, a[s][e]);  // exact
+            if (S32) left[s][e] = fma<BF>(v, rest, left[s][e]);
           }
         }
-        out[h][0] = make_uint4(a[0][0], a[0][2], a[1][0], a[1][2]);
-        out[h][1] = make_uint4(a[0][1], a[0][3], a[1][1], a[1][3]);
+        out[0][h][0] = make_uint4(a[0][0], a[0][2], a[1][0], a[1][2]);
+        out[0][h][1] = make_uint4(a[0][1], a[0][3], a[1][1], a[1][3]);
+        out[1][h][0] = make_uint4(left[0][0], left[0][2], left[1][0], left[1][2]);
+        out[1][h][1] = make_uint4(left[0][1], left[0][3], left[1][1], left[1][3]);
       }
       if (!mbar_wait_warp(empty + stage * 8, phase, abort_flag, kWaitNs, &g_q4_tc_error, kErrWork)) break;
       const unsigned row = st0 + stage * stage_bytes + (bl * 16 + g) * 128;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const unsigned at = static_cast<unsigned>((4 * (h ^ odd) + t) ^ g) << 4;
-        sts128(row + at, out[h][0].x, out[h][0].y, out[h][0].z, out[h][0].w);
-        sts128(row + 8 * 128 + at, out[h][1].x, out[h][1].y, out[h][1].z, out[h][1].w);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          sts128(row + i * kABytes + at, out[i][h][0].x, out[i][h][0].y, out[i][h][0].z, out[i][h][0].w);
+          sts128(row + i * kABytes + 8 * 128 + at, out[i][h][1].x, out[i][h][1].y, out[i][h][1].z, out[i][h][1].w);
+        }
       }
       if (GATHER) {
-        const unsigned b = st0 + stage * stage_bytes + kABytes;
+        const unsigned b = st0 + stage * stage_bytes + 2 * kABytes;
         for (int j0 = 0; j0 < p.n; j0 += 128) {
           if (j0) {
 #pragma unroll
@@ -274,7 +295,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_q4_tc_kernel(const __grid_
       for (; asked < n_st; ++asked) {
         if (!mbar_wait_parked(empty + stage * 8, phase, abort_flag, kWaitNs, &g_q4_tc_error, kErrLoad)) break;
         mbar_expect_tx(full_b + stage * 8, b_bytes);
-        tma_load_2d(st0 + stage * stage_bytes + kABytes, &map, ua * kUnitK + asked * kStageK, row0, full_b + stage * 8);
+        tma_load_2d(st0 + stage * stage_bytes + 2 * kABytes, &map, ua * kUnitK + asked * kStageK, row0, full_b + stage * 8);
         if (++stage == p.stages) stage = 0, phase ^= 1;
       }
     }
@@ -289,9 +310,13 @@ __global__ void __launch_bounds__(kThreads, 1) linear_q4_tc_kernel(const __grid_
         break;
       tc_fence_after();
       if (issuer) {
-        const unsigned long long a = desc_of(st0 + stage * stage_bytes), b = desc_of(st0 + stage * stage_bytes + kABytes);
+        const unsigned at = st0 + stage * stage_bytes;
+        const unsigned long long a = desc_of(at), left = desc_of(at + kABytes), b = desc_of(at + 2 * kABytes);
 #pragma unroll
-        for (int k = 0; k < kStageK / 16; ++k) umma_f16(tmem, a + k * 2, b + k * 2, idesc, it > 0 || k > 0 ? 1u : 0u);
+        for (int k = 0; k < kStageK / 16; ++k) {
+          umma_f16(tmem, a + k * 2, b + k * 2, idesc, it > 0 || k > 0 ? 1u : 0u);
+          umma_f16(tmem + p.n, left + k * 2, b + k * 2, idesc, it > 0 || k > 0 ? 1u : 0u);
+        }
         umma_commit(empty + stage * 8);
       }
       __syncwarp();
@@ -323,11 +348,15 @@ __global__ void __launch_bounds__(kThreads, 1) linear_q4_tc_kernel(const __grid_
     const float inverse = real ? 1.0f / p.power[o] : 0.0f, bias = real ? p.bias[o] : 0.0f;
     float* sums = reinterpret_cast<float*>(smem_raw + kHeader);  // [row][output]: the stages' place
     for (int c = (warp >> 2) * 16; c < p.n; c += kWorkers / 4 * 16) {
-      unsigned v[16];
+      unsigned v[16], left[16];
       tmem_ld16(tmem + (static_cast<unsigned>((warp & 3) * 32) << 16) + c, v);
+      tmem_ld16(tmem + (static_cast<unsigned>((warp & 3) * 32) << 16) + p.n + c, left);
       tmem_ld_wait16(v);
+      tmem_ld_wait16(left);
 #pragma unroll
       for (int j = 0; j < 16; ++j) {
+        // (an infinity in x times what is left of a weight, which may be 0 or of the other sign, is not to count)
+        if ((v[j] & 0x7f800000u) != 0x7f800000u) v[j] = __float_as_uint(__uint_as_float(v[j]) + __uint_as_float(left[j]));
         if (p.ks > 1) sums[(c + j) * kOuts + ol] = __uint_as_float(v[j]);
         else if (real && row0 + c + j < p.rows) store_y<BF>(p, row0 + c + j, o, fmaf(__uint_as_float(v[j]), inverse, bias));
       }
@@ -423,8 +452,8 @@ int launch_linear_q4_tc(const LinearQ4Call& c, const LinearQ4Layout& l, void* st
   p.n = static_cast<int>((c.rows + row_tiles - 1) / row_tiles + 15) / 16 * 16;
   row_tiles = (static_cast<long long>(c.rows) + p.n - 1) / p.n;
   p.tmem_cols = 32;
-  while (p.tmem_cols < p.n) p.tmem_cols *= 2;
-  const int rings = kWorkers * kRing * (l.record - kUnitWeights / 2), stage = kABytes + p.n * kStageK * 2;
+  while (p.tmem_cols < 2 * p.n) p.tmem_cols *= 2;
+  const int rings = kWorkers * kRing * (l.record - kUnitWeights / 2), stage = 2 * kABytes + p.n * kStageK * 2;
   p.stages = std::min(kMaxStages, (kSmem - kHeader - rings) / stage);
   const size_t smem = kHeader + std::max<size_t>(static_cast<size_t>(p.stages) * stage + rings, p.ks > 1 ? static_cast<size_t>(p.n) * kOuts * 4 : 0);
   const long long grid = p.m_tiles * row_tiles * p.ks;

@@ -27,6 +27,9 @@ inline int parts_of(int group) { return group % 128 == 0 ? 1 : group % 64 == 0 ?
 // Whether a layer's packed scales are 32 bits wide: those of 16 bits are kept where they are of the type its kernel computes in.
 inline bool wide_scales(int scale_dtype, int dtype) { return scale_dtype != (dtype == GI_F16 ? static_cast<int>(GI_F16) : static_cast<int>(GI_BF16)); }
 
+// Where an output's power of two brings its largest scale: in fp16 as far up as 15 times it allows, for the sake of the small ones.
+inline int power_top(int dtype) { return dtype == GI_F16 ? 12 : 0; }
+
 // bytes of a record, of what lies in front of its zero points
 __host__ __device__ constexpr int zeros_at(int parts, bool wide) { return kUnitWeights + parts * 16 * (wide ? 4 : 2); }
 __host__ __device__ constexpr int record_bytes(int parts, bool wide, bool zeros) {

@@ -419,3 +419,82 @@ def test_results_belong_to_the_stream_whose_handle_was_given():
     y = layer.run(x, stream=0)  # the default stream by its handle
     torch.cuda.synchronize()
     assert torch.equal(y, layer.run(x))
+
+
+# ---------------------------------------------------------------- more than 16 rows of a 16-bit type: weights in two parts
+def two_part_bound(x, weights, group, act="none"):
+    """(y, bound): ref.linear_q4's for weights that are not rounded (its form for up to 16 rows), and what two parts of x's type leave out
+    of a weight.  scale * (q - zero), with a scale in the type's digits D (8 or 11) and 4 digits of q - zero, has D + 4 of the 2 D + 1
+    digits of two parts: nothing is left out.  A scale in 32 bits is taken as two parts: off by 2^-2D of itself at most (half a step of the
+    second part, which is 2^-D of the first at most); its second part's product with q - zero and the second part of the weight are
+    rounded, each by 2^-D of at most 2^-D of the weight: 2^-2D for both together, and as much again for their sum.  So 4 2^-2D at most.
+    fp16: what lies below its smallest step 2^-24, where the output's largest scale is 2^11 or more: of two parts of a scale half a step,
+    15 times, of the weight's parts at most 2 steps: 17 steps or 2^-31 of that scale."""
+    q, s, z, _ = weights
+    parts = [ref.linear_q4(x[r:r + 16], *weights, group, act) for r in range(0, x.shape[0], 16)]
+    y, bound = torch.cat([p[0] for p in parts]), torch.cat([p[1] for p in parts])
+    digits = 8 if x.dtype == torch.bfloat16 else 11
+    more = 0.0
+    if s.dtype == torch.float32:
+        more = 4 * 2.0 ** (-2 * digits) * (x.double().abs() @ ref.q4_weights(q, s, z, x.shape[1], group).abs().t())
+    if x.dtype == torch.float16:
+        more = more + 2.0 ** -31 * x.double().abs().sum(1, keepdim=True) * s.double().abs().amax(1)
+    return y, bound + 1.01 * more
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("rows", [16, 17, 40, 130, 300])
+@pytest.mark.parametrize("scale", [torch.float16, torch.float32])
+def test_scales_of_one_output_far_apart(dtype, rows, scale):
+    """A group of large scales, which x passes over, beside groups of scales 2^25 times smaller."""
+    q, s, z, b = ref.q4_layer(2, 640, 150, 128, scale, zeros=True, bias=False)
+    s = (s.float() * 0.1).to(scale)
+    s[:, 1] = 30000.0
+    s[::2, 3] = 1e-3
+    layer = api.LinearQ4(q, s, z, cin=640, group=128, dtype=GI[dtype])
+    x = rows_of(rows, rows, 640, dtype)
+    x[:, 128:256] = 0
+    got = layer.run(x.cuda()).double().cpu()
+    want, bound = two_part_bound(x, (q, s, z, None), 128)
+    assert ((got - want).abs() <= bound).all(), ((got - want).abs() / bound).max()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("group", [32, 64, 96, 128, 160, 1024, 1 << 30])
+@pytest.mark.parametrize("dtype,scale", [(torch.float16, torch.float16), (torch.float16, torch.float32), (torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float16),
+                                         (torch.bfloat16, torch.float32)])
+@pytest.mark.parametrize("zeros", [False, True])
+def test_many_rows_keep_the_digits_of_weights(group, dtype, scale, zeros):
+    """One-hot rows: y is a weight itself, rounded once; and sums of 700 products."""
+    cin, cout = 700, 140
+    layer, w = make(group % 1000, cin, cout, group, dtype, scale, zeros, bias=False)
+    q, s, z, _ = w
+    hot = torch.zeros((cin, cin), dtype=dtype)
+    hot[torch.arange(cin), torch.arange(cin)] = 1.0
+    got = layer.run(hot.cuda()).cpu()
+    values = ref.q4_weights(q, s, z, cin, group).t()
+    if scale == torch.float32:
+        assert ((got.double() - values).abs() <= values.abs() * (ref.UNIT[dtype] + 4.1 * 2.0 ** (-16 if dtype == torch.bfloat16 else -22))).all()
+    else:
+        assert torch.equal(got, values.float().to(dtype))
+    for rows in (17, 33, 129, 256, 400):
+        x = rows_of(rows, rows, cin, dtype)
+        got = layer.run(x.cuda()).double().cpu()
+        want, bound = two_part_bound(x, w, group)
+        assert ((got - want).abs() <= bound).all(), (rows, ((got - want).abs() / bound).max())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("cin,cout", [(256, 300), (4096, 40)])
+def test_an_infinity_in_many_rows_gives_what_it_gives_in_few(dtype, cin, cout):
+    q, s, z, b = ref.q4_layer(4, cin, cout, 64, torch.float32)
+    layer = api.LinearQ4(q, s, z, b, cin=cin, group=64, dtype=GI[dtype])
+    x = rows_of(4, 40, cin, dtype)
+    x[3, 17], x[30, cin - 1], x[9, 0] = float("inf"), -float("inf"), float("nan")
+    got = layer.run(x.cuda()).cpu()
+    few = torch.cat([layer.run(x[r:r + 8].cuda()) for r in range(0, 40, 8)]).cpu()
+    assert torch.equal(torch.isnan(got), torch.isnan(few)) and torch.equal(torch.isinf(got), torch.isinf(few))
+    there = torch.isinf(few)
+    assert there.any() and torch.equal(got[there], few[there])
