@@ -41,7 +41,8 @@ using namespace frag;
 using namespace q4;
 
 // One CTA an SM: two of 8 warps would each stage x (8 rows 4096 -> 12288 13.0 us, two CTAs 15.2; 16 rows 8192 -> 8192 22.8 and 27.3;
-// one row 8192 -> 28672 31.4 and 33.1, 4096 -> 4096 5.9 and 5.5).
+// one row 8192 -> 28672 31.4 and 33.1, 4096 -> 4096 5.9 and 5.5).  That leaves 128 registers a thread: of the 48 variants of more than 8
+// columns 33 spill, by 32 bytes at most and by 108 where there are more than 16.
 constexpr int kWarps = 16, kThreads = kWarps * 32;
 // A warp's ring of copies: slots of two records (neighbours of one block, or one of each of two blocks).  16 warps keep 128 KB of
 // requests open.
@@ -87,10 +88,12 @@ __device__ __forceinline__ void mma(float (&d)[4], const unsigned (&a)[4], unsig
   else mma16816(d, a, b0, b1);
 }
 
-// Eight channels k .. k + 7 of row r of x (16-bit types), zero behind the last one.
+// Eight channels k .. k + 7 of row r of x (16-bit types), zero behind the last one.  GR: as an operator
+// of a graph - x and y may lie in slices of 4 channels, y may be joined with a residual; fp16 and up to 8 columns only.
+template <bool GR>
 __device__ __forceinline__ uint4 load_x8(const Params& p, int r, int k) {
   const unsigned short* x = static_cast<const unsigned short*>(p.x);
-  if (p.x_slice) {  // slices of 4 channels: the lanes behind the last channel hold zeros
+  if (GR && p.x_slice) {  // the lanes behind the last channel hold zeros
     const unsigned short* s = x + (k >> 2) * p.x_slice + r * 4ll;
     uint2 a = make_uint2(0u, 0u), b = a;
     if (k < p.cin) a = *reinterpret_cast<const uint2*>(s);
@@ -121,18 +124,18 @@ __device__ __forceinline__ void split3(float v, unsigned (&s)[3]) {
 }
 
 // Rows of x for units [u0, u0 + n) into shared memory, `pitch` bytes a row.
-template <int XT>
+template <int XT, bool GR>
 __device__ __forceinline__ void stage_x(const Params& p, unsigned char* xs, int pitch, int row0, int nrows, int u0, int n) {
   const int per_row = n * (kUnitK / 8);
   for (int i = threadIdx.x; i < per_row * nrows; i += kThreads) {
     int r = i / per_row, c = i - r * per_row;
-    if (p.x_slice) {  // the pixels of a slice are neighbours
+    if (GR && p.x_slice) {  // the pixels of a slice are neighbours
       c = i / nrows;
       r = i - c * nrows;
     }
     const int k = u0 * kUnitK + c * 8;
     if (XT != GI_F32) {
-      *reinterpret_cast<uint4*>(xs + r * pitch + c * 16) = load_x8(p, row0 + r, k);
+      *reinterpret_cast<uint4*>(xs + r * pitch + c * 16) = load_x8<GR>(p, row0 + r, k);
     } else {
       const float* x = static_cast<const float*>(p.x) + (row0 + r) * p.x_row + k;
       float v[8];
@@ -161,22 +164,22 @@ __device__ __forceinline__ float act_nan(float v, int act) {
   return v;
 }
 
-template <int XT>
+template <int XT, bool GR>
 __device__ __forceinline__ void store_y(const Params& p, int r, int o, float v) {
   v = act_nan(v, p.act_pre);
   long long at;
-  if (p.y_slice) {
+  if (GR && p.y_slice) {
     at = (o >> 2) * p.y_slice + r * 4ll + (o & 3);
   } else {
     long long row = r;
-    if (p.plane) {
+    if (GR && p.plane) {
       const int img = r / p.plane, in = r - img * p.plane;
       if (in >= p.real) return;
       row = static_cast<long long>(img) * p.real + in;
     }
     at = row * p.y_row + o;
   }
-  if (p.has_res) v = act_nan(v + __half2float(static_cast<const __half*>(p.res)[(o >> 2) * p.res_slice + r * 4ll + (o & 3)]), p.act_post);
+  if (GR && p.has_res) v = act_nan(v + __half2float(static_cast<const __half*>(p.res)[(o >> 2) * p.res_slice + r * 4ll + (o & 3)]), p.act_post);
   if (XT == GI_F16) static_cast<__half*>(p.y)[at] = __float2half_rn(v);
   else if (XT == GI_BF16) static_cast<__nv_bfloat16*>(p.y)[at] = __float2bfloat16_rn(v);
   else static_cast<float*>(p.y)[at] = v;
@@ -187,7 +190,7 @@ __device__ __forceinline__ void store_y(const Params& p, int r, int o, float v) 
 template <int XT, int NT, int RB, int HG, bool ZP, bool S32>
 __global__ void __launch_bounds__(kThreads, 1) linear_q4_kernel(const Params p) {
   extern __shared__ __align__(128) unsigned char smem[];
-  constexpr bool BF = XT != GI_F16;
+  constexpr bool BF = XT != GI_F16, kGraph = XT == GI_F16 && NT == 1;
   constexpr int kCols = XT == GI_F32 ? 3 : 1;  // columns of a row of x
   constexpr int kZerosAt = zeros_at(HG, S32), kRecord = record_bytes(HG, S32, ZP), kBehind = kRecord - kUnitWeights;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -195,7 +198,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_q4_kernel(const Params p) 
   const int nrows = min(p.row_tile, p.rows - row0), cols = nrows * kCols;
   const int n_blocks = (p.cout + 15) / 16, n_sets = (n_blocks + RB - 1) / RB;
   // A tile's sets of RB blocks are cut into items: one set and one of kw parts of the CTA's share of the input channels.  Warp w
-  // takes the items w, w + 8, ..., one after the other; each leaves its sum in shared memory.
+  // takes the items w, w + 16, ..., one after the other; each leaves its sum in shared memory.
   const int set0 = static_cast<int>(static_cast<long long>(n_sets) * tile / p.tiles), sets = static_cast<int>(static_cast<long long>(n_sets) * (tile + 1) / p.tiles) - set0;
   const int items = sets * p.kw;
   constexpr int kSteps = 2 / RB;  // records of a block that are one step
@@ -330,7 +333,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_q4_kernel(const Params p) 
   unsigned from = ring;
   for (int c = 0; c < chunks; ++c) {
     if (c) __syncthreads();  // every warp is done with the chunk before
-    stage_x<XT>(p, smem, pitch, row0, nrows, ua + c * p.chunk, min(p.chunk, ub - ua - c * p.chunk));
+    stage_x<XT, kGraph>(p, smem, pitch, row0, nrows, ua + c * p.chunk, min(p.chunk, ub - ua - c * p.chunk));
     __syncthreads();
     for (int item = warp; item < items; item += kWarps) {
       int first, last;
@@ -392,7 +395,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_q4_kernel(const Params p) 
     const int r = i / outs, ol = i - r * outs, o = set0 * RB * 16 + ol;
     if (o >= p.cout) {
       // the channels that complete the last slice are zeros
-      if (p.y_slice && o < (p.cout + 3) / 4 * 4) static_cast<__half*>(p.y)[(o >> 2) * p.y_slice + (row0 + r) * 4ll + (o & 3)] = __float2half_rn(0.0f);
+      if (kGraph && p.y_slice && o < (p.cout + 3) / 4 * 4) static_cast<__half*>(p.y)[(o >> 2) * p.y_slice + (row0 + r) * 4ll + (o & 3)] = __float2half_rn(0.0f);
       continue;
     }
     const int bl = ol >> 4;
@@ -413,7 +416,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_q4_kernel(const Params p) 
         }
       }
     }
-    store_y<XT>(p, row0 + r, o, v);
+    store_y<XT, kGraph>(p, row0 + r, o, v);
   }
   if (p.ks > 1) cluster_sync();  // nobody leaves while its shared memory is read
 }
@@ -527,15 +530,14 @@ struct Shape {
 // parts (kw) of a CTA's share of a sum.
 Shape choose_shape(int rows, int cols_per_row, int n_blocks, int n_units, int sms) {
   Shape s{};
-  const int fit = 32 / cols_per_row;
-  s.row_tile = std::min(rows, fit);
+  s.row_tile = std::min(rows, cols_per_row == 1 ? 16 : 32 / cols_per_row);
   const int cols = s.row_tile * cols_per_row;
   s.nt = cols <= 8 ? 1 : cols <= 16 ? 2 : 4;
   s.rb = s.nt == 1 ? 1 : 2;
   const int n_sets = (n_blocks + s.rb - 1) / s.rb;
-  // More than 8 columns: pairs of CTAs share x out among themselves, each stages half of its channels (16 rows 8192 -> 8192 22.8 us,
-  // alone 28.5; 8 rows 4096 -> 12288 13.0 and 12.9).  Few outputs of many channels: more CTAs share a sum, as long as each has 2048
-  // channels of it - 512 of more than 8 columns (4 rows 16384 -> 512: 8 CTAs 7.5 us, 4 7.6, 1 35; 12 rows 1280 -> 1001: 2 4.5, 4 5.6;
+  // More than 8 columns: pairs of CTAs share x out among themselves, each stages half of its channels, whatever their number (16 rows
+  // 8192 -> 8192 22.8 us, alone 28.5; 8 rows 4096 -> 12288 13.0 and 12.9).  Few outputs of many channels: while that leaves SMs idle, twice
+  // as many CTAs share a sum if each then has 2048 channels of it or more - 512 of more than 8 columns (4 rows 16384 -> 512: 8 CTAs 7.5 us, 4 7.6, 1 35; 12 rows 1280 -> 1001: 2 4.5, 4 5.6;
   // one row 1280 -> 1001: 1 CTA 2.9, 2 3.5).
   const bool many = cols > 8;
   s.ks = many && n_units >= 2 ? 2 : 1;
@@ -557,11 +559,12 @@ Shape choose_shape(int rows, int cols_per_row, int n_blocks, int n_units, int sm
 
 template <int XT, bool S32>
 cudaError_t launch_type(const Params& p, const Shape& s, int parts, bool zeros, unsigned grid, size_t smem, cudaStream_t stream) {
-  switch (s.nt) {
-    case 1: return launch_shape<XT, 1, 1, S32>(p, parts, zeros, grid, smem, stream);
-    case 2: return launch_shape<XT, 2, 2, S32>(p, parts, zeros, grid, smem, stream);
-    default: return launch_shape<XT, 4, 2, S32>(p, parts, zeros, grid, smem, stream);
+  if (s.nt == 1) return launch_shape<XT, 1, 1, S32>(p, parts, zeros, grid, smem, stream);
+  // (16 rows of a 16-bit type are two eights: more of them go to tcgen05)
+  if constexpr (XT == GI_F32) {
+    if (s.nt == 4) return launch_shape<XT, 4, 2, S32>(p, parts, zeros, grid, smem, stream);
   }
+  return launch_shape<XT, 2, 2, S32>(p, parts, zeros, grid, smem, stream);
 }
 
 // a caller's scale in 32 bits: exact
@@ -715,6 +718,8 @@ int launch_linear_q4(const LinearQ4Call& c, void* stream) {
   if (linear_q4_tc_wanted(c)) return launch_linear_q4_tc(c, l, stream);
   const int cols_per_row = c.dtype == GI_F32 ? 3 : 1;
   const Shape s = choose_shape(c.rows, cols_per_row, l.n_blocks, l.n_units, device_sm_count());
+  const bool graph = c.x_slice || c.y_slice || c.plane || c.ep.has_res;
+  if (graph && (c.dtype != GI_F16 || s.nt != 1)) return static_cast<int>(cudaErrorInvalidConfiguration);  // (a graph brings 8 rows of fp16 at most)
   Params p{};
   const unsigned char* blob = static_cast<const unsigned char*>(c.blob);
   p.wts = blob;
