@@ -746,7 +746,7 @@ int launch_linear_q4(const LinearQ4Call& c, void* stream) {
   // shared memory: x (as much of it as there is room for), the rings of copies, the items' sums
   const int n_sets = (l.n_blocks + s.rb - 1) / s.rb, sets = (n_sets + s.tiles - 1) / s.tiles;
   const int rings = kWarps * kSlots * 2 * l.record, sums = sets * s.kw * s.rb * cols * 16 * 4;
-  const int fit = ((kSmem - rings - sums) / cols - 64) / (kUnitK * 2);
+  const int fit = ((kSmem - rings - sums - 64) / cols - 64) / (kUnitK * 2);  // (all are whole 64 bytes, the rings begin at 128)
   const int need = (l.n_units + s.ks - 1) / s.ks, step = 2 / s.rb;
   p.chunk = std::max(1, std::min(fit / step, (need + step - 1) / step)) * step;
   p.ring_at = (cols * (p.chunk * kUnitK * 2 + 64) + 127) / 128 * 128;

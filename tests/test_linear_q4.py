@@ -498,3 +498,21 @@ def test_an_infinity_in_many_rows_gives_what_it_gives_in_few(dtype, cin, cout):
     assert torch.equal(torch.isnan(got), torch.isnan(few)) and torch.equal(torch.isinf(got), torch.isinf(few))
     there = torch.isinf(few)
     assert there.any() and torch.equal(got[there], few[there])
+
+
+@pytest.mark.gpu
+def test_a_layer_whose_rows_fill_shared_memory_to_the_last_byte():
+    """One row of 64000 channels to 33168 outputs: what is staged of x, the rings and the sums end at a CTA's limit."""
+    cin, cout, group = 64000, 33168, 128
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q = torch.randint(0, 256, (cout, cin // 2), dtype=torch.uint8, device="cuda", generator=g)
+    s = torch.rand((cout, cin // group), device="cuda", generator=g).add_(0.5).half()
+    layer = api.LinearQ4(q, s, cin=cin, group=group)
+    x = torch.zeros((1, cin), dtype=torch.float16, device="cuda")
+    want = torch.zeros((cout,), dtype=torch.float64, device="cuda")
+    for k, v in ((0, 1.0), (127, -2.0), (31999, 0.5), (32000, 3.0), (51235, 1.5), (63999, -1.0)):
+        x[0, k] = v
+        want += v * ((q[:, k // 2] >> (4 * (k % 2)) & 15).double() - 8) * s[:, k // group].double()
+    got = layer.run(x)[0].double()
+    # six products, a rounding of each sum in fp32; half a step of the result
+    assert ((got - want).abs() <= want.abs() * 2.0 ** -11 + 6 * 6 * 8 * 1.5 * 3 * 2.0 ** -23).all()
