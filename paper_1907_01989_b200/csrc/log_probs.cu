@@ -169,11 +169,12 @@ __device__ __forceinline__ Stat warp_merge(Stat st, float c, int width) {
 }
 
 // log p of a logit, given a row's sums: minus infinity in a row in which nothing is left
+template <int XT>
 __device__ __forceinline__ float log_prob(float v, const Stat& st, float log_s, float inv_t) {
   if (st.s == 0.0f) return -INFINITY;
   float d = (v - st.m) * inv_t;
   // two numbers whose difference is none in fp32: halves of them, which the temperature may bring back into its range
-  if (d == -INFINITY) d = 2.0f * ((0.5f * v - 0.5f * st.m) * inv_t);
+  if (XT != GI_F16 && d == -INFINITY) d = 2.0f * ((0.5f * v - 0.5f * st.m) * inv_t);
   return d - log_s;
 }
 __device__ __forceinline__ float entropy_of(const Stat& st, float log_s) { return st.s == 0.0f ? 0.0f : log_s - st.t * kLn2 / st.s; }
@@ -311,13 +312,15 @@ struct Seen {
   }
 };
 
+template <int XT>
 __device__ __forceinline__ void write_given(const Params& p, long long row, int j, const Stat& st, float log_s, float v, int id) {
   // (the logit is read by the caller where the class is one of the row's)
-  p.given_lp[row * p.n_given + j] = id < 0 ? 0.0f : id >= p.classes ? __int_as_float(0x7fffffff) : log_prob(v, st, log_s, p.inv_t);
+  p.given_lp[row * p.n_given + j] = id < 0 ? 0.0f : id >= p.classes ? __int_as_float(0x7fffffff) : log_prob<XT>(v, st, log_s, p.inv_t);
 }
+template <int XT>
 __device__ __forceinline__ void write_top(const Params& p, long long row, int j, u64 key, const Stat& st, float log_s) {
   p.top_ids[row * p.top + j] = class_of(key);
-  p.top_lp[row * p.top + j] = log_prob(value_of(key), st, log_s, p.inv_t);
+  p.top_lp[row * p.top + j] = log_prob<XT>(value_of(key), st, log_s, p.inv_t);
 }
 
 // ---------------------------------------------------------------- a CTA, or a cluster of them, for a row
@@ -496,11 +499,11 @@ __global__ void __launch_bounds__(T) row_kernel(const Params p) {
     const Stat st = sh.st;
     const float log_s = logf(st.s);
     if (tid == 0 && p.entropy) p.entropy[r] = entropy_of(st, log_s);
-    if (tid < p.top) write_top(p, r, tid, sh.best[tid], st, log_s);
-    if (tid < p.n_given) write_given(p, r, tid, st, log_s, given0, id0);
+    if (tid < p.top) write_top<XT>(p, r, tid, sh.best[tid], st, log_s);
+    if (tid < p.n_given) write_given<XT>(p, r, tid, st, log_s, given0, id0);
     for (int j = tid + kThreads; j < p.n_given; j += kThreads) {
       const int id = p.given[r * p.n_given + j];
-      write_given(p, r, j, st, log_s, id >= 0 && id < p.classes ? row.at(id) : 0.0f, id);
+      write_given<XT>(p, r, j, st, log_s, id >= 0 && id < p.classes ? row.at(id) : 0.0f, id);
     }
   }
   if (p.ks > 1) cluster_sync();  // nobody leaves while its shared memory is read
@@ -534,17 +537,17 @@ __global__ void __launch_bounds__(kThreads) warp_kernel(const Params p) {
   const Stat st = warp_merge(seen.stat(), p.c, 32);
   const float log_s = logf(st.s);
   if (lane == 0 && p.entropy) p.entropy[r] = entropy_of(st, log_s);
-  if (lane < p.n_given) write_given(p, r, lane, st, log_s, given0, id0);
+  if (lane < p.n_given) write_given<XT>(p, r, lane, st, log_s, given0, id0);
   for (int j = lane + 32; j < p.n_given; j += 32) {
     const int id = p.given[r * p.n_given + j];
-    write_given(p, r, j, st, log_s, id >= 0 && id < p.classes ? row.at(id) : 0.0f, id);
+    write_given<XT>(p, r, j, st, log_s, id >= 0 && id < p.classes ? row.at(id) : 0.0f, id);
   }
   if (p.top == 0) return;
   if (p.top == 1) {
     u64 mine = seen.best(row);
 #pragma unroll
     for (int o = 16; o; o >>= 1) mine = max64(mine, shfl_xor64(mine, o));
-    if (lane == 0) write_top(p, r, 0, mine, st, log_s);
+    if (lane == 0) write_top<XT>(p, r, 0, mine, st, log_s);
     return;
   }
   // The least of the `top` leading lanes' largest values bounds the answer from below (equal values count together); a lane without
@@ -584,7 +587,7 @@ __global__ void __launch_bounds__(kThreads) warp_kernel(const Params p) {
       const u64 key = found[k];
       int place = 0;
       for (int j = 0; j < n; ++j) place += found[j] > key;
-      if (place < p.top) write_top(p, r, place, key, st, log_s);
+      if (place < p.top) write_top<XT>(p, r, place, key, st, log_s);
     }
     return;
   }
@@ -604,7 +607,7 @@ __global__ void __launch_bounds__(kThreads) warp_kernel(const Params p) {
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) best = max64(best, shfl_xor64(best, o));
-    if (lane == 0) write_top(p, r, k, best, st, log_s);
+    if (lane == 0) write_top<XT>(p, r, k, best, st, log_s);
     last = best;
   }
 }
@@ -700,7 +703,7 @@ __global__ void __launch_bounds__(kThreadRows) thread_kernel(const Params p) {
   if (p.entropy) p.entropy[r] = entropy_of(st, log_s);
   for (int j = 0; j < p.n_given; ++j) {
     if (j) id = p.given[r * p.n_given + j];
-    write_given(p, r, j, st, log_s, id >= 0 && id < p.classes ? Elem<XT>::f32(mine[id]) : 0.0f, id);
+    write_given<XT>(p, r, j, st, log_s, id >= 0 && id < p.classes ? Elem<XT>::f32(mine[id]) : 0.0f, id);
   }
   if (p.top) {
   int where = 0;  // the first of the largest
@@ -711,7 +714,7 @@ __global__ void __launch_bounds__(kThreadRows) thread_kernel(const Params p) {
     for (int j = MOST - 1; j >= 0; --j) where = v[j] != v[j] ? j : where;
   }
   p.top_ids[r * p.top] = where;
-  p.top_lp[r * p.top] = log_prob(high, st, log_s, p.inv_t);
+  p.top_lp[r * p.top] = log_prob<XT>(high, st, log_s, p.inv_t);
   if (p.top > 1) {
   if (XT != GI_F32) {
     // the ordered bits of a value of 16 bits leave at least 13 low ones to themselves: the class goes there
@@ -725,7 +728,7 @@ __global__ void __launch_bounds__(kThreadRows) thread_kernel(const Params p) {
       for (int j = 0; j < MOST; ++j) best = max(best, key[j] < last ? key[j] : static_cast<int>(0x80000000u));
       const int id = kFew - 1 - (best & (kFew - 1));
       p.top_ids[r * p.top + k] = id;
-      p.top_lp[r * p.top + k] = log_prob(Elem<XT>::f32(mine[id]), st, log_s, p.inv_t);
+      p.top_lp[r * p.top + k] = log_prob<XT>(Elem<XT>::f32(mine[id]), st, log_s, p.inv_t);
       last = best;
     }
   } else {
@@ -736,7 +739,7 @@ __global__ void __launch_bounds__(kThreadRows) thread_kernel(const Params p) {
         const u64 key = key_of(Elem<XT>::f32(mine[j]), j);
         if (key < last) best = max64(best, key);
       }
-      write_top(p, r, k, best, st, log_s);
+      write_top<XT>(p, r, k, best, st, log_s);
       last = best;
     }
   }
