@@ -344,6 +344,8 @@ class LinearQ4:
     def run(self, x, y=None, stream=None):
         """y[..., cout] = act(x[..., cin] w^T + bias) on `stream` (default: the current one of the layer's device); y is made where none is given.
         Two axes may have any distance between rows; other tensors are contiguous."""
+        if self.device.type != "cuda":
+            raise ValueError(f"the layer is in host memory: need one on a CUDA device ({self.device})")
         if y is None:
             import torch
             with _allocating_on(stream, self.device):

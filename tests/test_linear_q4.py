@@ -516,3 +516,14 @@ def test_a_layer_whose_rows_fill_shared_memory_to_the_last_byte():
     got = layer.run(x)[0].double()
     # six products, a rounding of each sum in fp32; half a step of the result
     assert ((got - want).abs() <= want.abs() * 2.0 ** -11 + 6 * 6 * 8 * 1.5 * 3 * 2.0 ** -23).all()
+
+
+def test_a_layer_in_host_memory_is_not_run():
+    """It can be packed there (and copied elsewhere); a launch would read host pointers."""
+    layer, _ = make(6, 96, 40, 32, torch.float16, device="cpu")
+    x = torch.zeros((4, 96), dtype=torch.float16)
+    for stream in (None, 0):
+        with pytest.raises(ValueError, match="CUDA"):
+            layer.run(x, torch.empty((4, 40), dtype=torch.float16), stream=stream)
+        with pytest.raises(ValueError, match="CUDA"):
+            layer.run(x, stream=stream)
