@@ -383,10 +383,12 @@ def log_probs(logits, given=None, top: int = 0, temperature: float = 1.0, out: O
     contiguous) -> log probabilities of `given` (int32 [..., n], negative: nothing asked), entropy and the `top` leading classes of
     each row, in `out` (log_probs_out; what is not asked for is left as it is there, and None in the result) or in new tensors."""
     import torch
-    classes = logits.shape[-1]
     device = logits.device
     if device.type != "cuda":
         raise ValueError("logits: need a tensor on a CUDA device")
+    if not logits.shape or not logits.shape[-1]:
+        raise ValueError(f"logits: need [..., classes] with at least one class, got {tuple(logits.shape)}")
+    classes = logits.shape[-1]
     ptr, ld, rows = _rows(logits, "logits", logits.dtype, classes, device)
     n_given = 0 if given is None else given.shape[-1]
     if out is None:

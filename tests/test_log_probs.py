@@ -365,3 +365,10 @@ def test_logits_whose_difference_is_beyond_fp32(dtype, rows, classes):
         assert torch.isfinite(got.top).all()
     got = api.log_probs(x.cuda(), given.cuda(), 4, 1.0)  # here it is not
     assert (got.given[:, 0] == -INF).all() and (got.given[:, 3] == 0).all()
+
+
+@pytest.mark.gpu
+def test_logits_without_classes_are_refused():
+    for shape in ((), (0,), (4, 0), (2, 2, 0)):
+        with pytest.raises((ValueError, api.GiError)):
+            api.log_probs(torch.zeros(shape, dtype=torch.float16, device="cuda"))
