@@ -37,6 +37,8 @@ class HostPipeline:
         if top:
             if len(output_shapes) != 1:
                 raise ValueError("answers need an executable with one output, the logits")
+            if not 0 < top <= min(api.GI_MAX_TOP, output_shapes[0][-1]):
+                raise ValueError(f"top: 1 .. {min(api.GI_MAX_TOP, output_shapes[0][-1])}, got {top}")
             rows = self.outs[0][0].numel() // output_shapes[0][-1]
             self.answers = [api.log_probs_out(rows, 0, top, device) for _ in range(slots)]
         self.loaded = [torch.cuda.Event() for _ in range(slots)]   # slot's inputs have arrived
@@ -74,6 +76,11 @@ class HostPipeline:
         """Enqueue one batch: pinned host tensors in, pinned host tensors out.  Asynchronous; results are
         complete after `synchronize()` (or after the compute stream reaches a later event)."""
         torch = self.torch
+        if self.top:
+            a = self.answers[0]
+            want = [(tuple(d.shape), d.dtype) for d in (a.top, a.top_ids, a.entropy)]
+            if [(tuple(h.shape), h.dtype) for h in host_outputs] != want:
+                raise ValueError(f"host_outputs: need buffers for the answers, {want}")
         s = self.n % self.slots
         self.n += 1
         with torch.cuda.stream(self.copy):

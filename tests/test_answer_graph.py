@@ -241,3 +241,27 @@ def test_captured_behind_work_of_two_streams():
         torch.cuda.synchronize()
         assert torch.equal(y, want_y) and torch.equal(e, want_y)
         assert all(torch.equal(p, r) for p, r in zip(out[1:], want[1:]))
+
+
+@pytest.mark.gpu
+def test_pipeline_refuses_buffers_that_are_not_its_answers():
+    """Three buffers of the answers' shapes and types: anything else would be left out, cast or stretched without a word."""
+    import torch
+    from paper_1907_01989_b200.pipeline import HostPipeline
+    spec = q4_graph(2, 1, 1, 64, 30)
+    ex = api.graph_from_spec(spec, api.GI_F16)[0].compile()
+    ex.bind("cuda:0")
+    pipe = HostPipeline(ex, [(2, 1, 1, 64)], [(2, 1, 1, 30)], torch.float16, "cuda:0", top=3)
+    x = torch.zeros((2, 1, 1, 64)).half().pin_memory()
+    good = [torch.empty((2, 3)).pin_memory(), torch.empty((2, 3), dtype=torch.int32).pin_memory(), torch.empty((2,)).pin_memory()]
+    for bad in (good[:2], good + good[:1], [good[1], good[0], good[2]], [good[0], good[1], torch.empty((2, 1)).pin_memory()],
+                [torch.empty((4, 3)).pin_memory()[:2].t().contiguous().t(), torch.empty((3,), dtype=torch.int32), good[2]]):
+        with pytest.raises(ValueError):
+            pipe.submit([x], bad)
+    pipe.submit([x], good)
+    pipe.synchronize()
+    assert torch.isfinite(good[0]).all() and (good[1] >= 0).all()
+    with pytest.raises(ValueError):
+        HostPipeline(ex, [(2, 1, 1, 64)], [(2, 1, 1, 30)], torch.float16, "cuda:0", top=31)
+    with pytest.raises(ValueError):
+        HostPipeline(ex, [(2, 1, 1, 64)], [(2, 1, 1, 30)], torch.float16, "cuda:0", top=33)
