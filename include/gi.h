@@ -345,7 +345,7 @@ GI_API gi_status gi_run_timed(gi_exec* e, const void* const* dev_inputs, void* c
 
 /* Health word of the device-side waits.  The tensor-core kernel waits on copy and MMA
  * completion with a limit of about one second per wait; a wait that runs out sets a bit here
- * (1 producer, 2 MMA issuer, 4 epilogue, 8 drain; 0x10000 depthwise staging copy;
+ * (1 producer, 2 MMA issuer, 4 epilogue, 8 drain, those of the 4-bit layers' kernel for many rows too; 0x10000 depthwise staging copy;
  * 0x100000 / 0x200000 / 0x400000 gather / MMA issuer / epilogue of the k x k tensor-core kernels; 0x1000000..0x8000000
  * producer / MMA issuer / data warps / drain of the lane-per-pixel 1x1 kernel; 0x10000000..
  * 0x80000000 copy warp / MMA issuer / compute warps / drain of the depthwise + pointwise kernel; 0x20000 / 0x40000 / 0x80000
@@ -391,7 +391,7 @@ GI_API gi_status gi_slice8_pointwise_run(const void* dev_in, void* dev_out, cons
  * Operators on rows: device tensors [rows][channels] whose channels are contiguous and whose rows are `ld` elements apart.  They
  * need no graph; a graph reaches the first one by GI_Q4 weights.  Like gi_run they enqueue on `stream` and return; they allocate
  * nothing, keep nothing between calls and give bit-identical outputs for the same inputs.  Any number of calls may run at once on
- * any streams.  Pointers belong to the current device and need the alignment of their elements only (blobs: 256 bytes).  Nothing
+ * any streams, from any threads.  Rows are at most 2^30 elements apart.  Pointers belong to the current device and need the alignment of their elements only (blobs: 256 bytes).  Nothing
  * is launched if an argument check fails. */
 
 /* Fully connected layer with 4-bit weights:
@@ -450,7 +450,8 @@ typedef struct gi_log_probs_desc {
   int32_t top;            /* 0 .. GI_MAX_TOP, at most `classes` */
 } gi_log_probs_desc;
 
-/* dev_given [rows][n_given] and the outputs are contiguous; those of 0 columns may be NULL, and so may dev_entropy. */
+/* dev_given [rows][n_given] and the outputs are contiguous; those of 0 columns may be NULL, and so may dev_entropy.  Outputs overlap neither
+ * one another nor the inputs. */
 GI_API gi_status gi_log_probs(const gi_log_probs_desc* desc, const void* dev_logits, const int32_t* dev_given, float* dev_given_log_probs,
                               float* dev_entropy, int32_t* dev_top_ids, float* dev_top_log_probs, void* stream);
 

@@ -55,8 +55,8 @@ static Loc loc_of(const gi_exec* e, int t) {
 }
 
 // Stored pixels up to which a 1x1 convolution runs on its 4-bit weights: a batch of 4 behind a pooling (a stored plane holds two
-// pixels at least).  Graphs of one such layer, weights not in L2, 4-bit against fp16 kernel: 1280 -> 1001 on 2 pixels 4.7 and 7.0 us,
-// on 8 7.0 and 6.9, on 16 9.6 and 8.1; 4096 -> 4096 on 2 8.1 and 25.5, on 8 14.2 and 17.5, on 16 22.8 and 20.8.
+// pixels at least).  Graphs of one such layer, weights not in L2, 4-bit against fp16 kernel: 1280 -> 1001 on 2 pixels 4.2 and 6.8 us,
+// on 8 6.6 and 7.5, on 16 9.3 and 8.8; 4096 -> 4096 on 2 8.4 and 20.2, on 8 13.9 and 17.8, on 16 20.1 and 21.1.
 constexpr long long kQ4Pixels = 8;
 
 // Weights of the CUDA-core convolution kernel: float W[group][tap][in_slice][32 co][4 ci],

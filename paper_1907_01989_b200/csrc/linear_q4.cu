@@ -9,10 +9,11 @@
 // fp32 for each group of input channels and are scaled in fp32: nothing of a weight is rounded.  For so few columns tcgen05 would
 // only add a store to shared memory for every weight; from 17 rows on it wins (linear_q4_tc.cu).
 //
-// Measured (B200): one row 8192 -> 28672 31.4 us, 3.9 TB/s (its copies alone 23 us, its arithmetic alone 27), one row 4096 -> 4096
-// 5.9 us, 8 rows 4096 -> 12288 13 us, 16 rows 5120 -> 13824 23 us.
+// Measured (B200): one row 8192 -> 28672 32 us, 3.7 TB/s (its copies alone 23 us, its arithmetic alone 27), one row 4096 -> 4096
+// 5.9 us, 8 rows 4096 -> 12288 13.5 us, 16 rows 5120 -> 13824 with zero points 23.5 us.
 //
 // x in 32 bits: a value is the exact sum of three bf16 numbers (8 + 8 + 8 digits), so a row of x becomes three columns of the product.
+// Ten rows are a tile, and every tile reads and expands all weights: 5 rows 4096 -> 12288 17 us, 10 47, 32 124, 256 755.
 //
 // Layout of the packed weights (linear_q4_pack): records of 16 outputs x 128 input channels, those of 16 outputs one after another.
 // A record is 1024 bytes of weights - lane l = 4 g + t of a warp reads bytes 16 l .. and 512 + 16 l .., which are rows g and g + 8,

@@ -5,20 +5,22 @@
 // channels).  Here a CTA computes 128 outputs x up to 256 rows: the weights are the A operand - sixteen warps, two for each block of 16
 // outputs, expand the records that their own rings of copies bring, scale them and store them to shared memory in the swizzled
 // layout (rows of 64 channels = 128 bytes, 16-byte units exchanged by the row's number) - and the rows of x the B operand, copied by
-// one thread as tiles of the same layout (rows that are not in whole 16-byte units are loaded by the expanding warps instead).  One thread issues the products, 128 x N x 16 each; the sums stay in tensor memory until
-// the last channel.  Expanding a record of 16 x 128 weights is shared by all rows of the tile.  Where outputs are few, the CTAs of a
-// cluster share the input channels and add their sums up through distributed shared memory, in a fixed order.
+// one thread as tiles of the same layout (rows that are not in whole 16-byte units are loaded by the expanding warps instead).  One thread
+// issues the products, 128 x N x 16 each; the sums stay in tensor memory until the last channel.  Expanding a record of 16 x 128 weights is
+// shared by all rows of the tile.  Where outputs are few, the CTAs of a cluster share the input channels and add their sums up through
+// distributed shared memory, in a fixed order.
 //
 // Precision: scale * (q - zero) enters as the sum of two numbers of x's type, the nearest one and what that leaves, each with a product and
 // a sum of its own (where the first sum is no number, the second does not count: what is left may be 0 or of the other sign).  For scales
-// in 16 bits (times 4 bits of q - zero) the two are all of it; of a scale in 32 bits, which enters in two parts as well, 16 digits or more
-// are left in bf16, 22 in fp16.  fp16 lacks range: a power of two for each output brings its largest scale to 2^11 .. 2^12, where 15 times
-// it is still a number; what lies below the smallest step there is 2^-31 of that scale at most.  Weights rounded once would take 24.7
-// instead of 31.4 us for 32 rows and 35 instead of 51 for 256.  q - zero alone, exact, needs sums of its own for each group, which
-// the sixteen warps have to read out of tensor memory, scale and add up: 35 us for 32 rows, 78 for 256, with groups of 32 50 and 113.
+// in 16 bits (times 4 bits of q - zero) the two are all of it; of a scale in 32 bits, which enters in two parts as well, at least 14 digits
+// are left in bf16 (16 were the fewest of 200 000), 20 in fp16 (22).  fp16 lacks range: a power of two for each output brings its largest
+// scale to 2^11 .. 2^12, where 15 times it is still a number; what lies below the smallest step there is 2^-31 of that scale at most.
+// Weights rounded once would take 24.8 instead of 31.7 us for 32 rows and 35 instead of 51 for 256.  q - zero alone, exact, needs sums of
+// its own for each group, which the sixteen warps have to read out of tensor memory, scale and add up: 35 us for 32 rows, 78 for 256, with
+// groups of 32 50 and 113.
 //
 // Measured (B200, 4096 -> 12288): 256 rows 51 us, 1024 rows 147 - two products for each weight, 1.0 and 1.4 PFLOP/s of them, the
-// former on 96 of the 148 SMs - 32 rows 31.4 us, bound by the expansion, and 256 rows 4096 -> 4096 23 us with 4 CTAs to a sum.
+// former on 96 of the 148 SMs - 32 rows 31.7 us, bound by the expansion, and 256 rows 4096 -> 4096 23 us with 4 CTAs to a sum.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>

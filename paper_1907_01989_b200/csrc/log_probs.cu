@@ -12,8 +12,9 @@
 // that do reach it are collected in shared memory and ranked by counting.  An element is a whole number of 64 bits, the value's
 // ordered bits above the inverted class, so that all are different and no order of execution shows.
 //
-// Measured (B200): 2048 x 131072 fp16 124 us (4.3 TB/s), without `top` 105 us (5.1); 4.2 M rows of 21 classes 87 us (3.0); 1 x 262144
-// fp32 9.7 us, 1 x 1001 5 us.
+// Measured (B200): 2048 x 131072 fp16 125 us (4.3 TB/s), without `top` 111 us (4.9); 50000 x 3000 152 us, without `top` 74; 4.2 M rows of
+// 21 classes 87 us (3.0), of 16 97, of 32 299, of 64 1017 (rows an even number of 32-bit words apart meet in the same banks of shared
+// memory); 1 x 262144 fp32 10 us, 1 x 1001 5 us.
 //
 // Three shapes: a thread a row for a handful of classes (every pixel of a segmentation), a warp a row (few classes, or many rows), a CTA a row - or a cluster
 // of up to 8 CTAs, where rows are few: they read one row together and join through distributed shared memory, in a fixed order.
@@ -777,8 +778,8 @@ cudaError_t launch_type(Params& p, cudaStream_t stream) {
     }
     return launch_pdl(k, dim3(grid), dim3(kThreadRows), smem, stream, static_cast<const Params>(p));
   }
-  // A warp a row: few classes, or enough rows to fill the GPU with warps (fp16, top 5: 5000 x 5000 31 us, with a CTA a row 46; 50000 x
-  // 3000 151 and 458; but 1200 x 5000 19 and 14, 20000 x 10000 fp32 385 and 281).
+  // A warp a row: few classes, or enough rows to fill the GPU with warps (fp16, top 5: 5000 x 5000 31 us, with a CTA a row 45; 50000 x
+  // 3000 146 and 452; but 1200 x 5000 17 and 14, 20000 x 10000 fp32 340 and 220).
   if (p.classes <= 2048 || (p.classes / V <= 1024 && p.rows >= 16 * sms)) {
     const unsigned grid = static_cast<unsigned>((static_cast<long long>(p.rows) + kWarps - 1) / kWarps);
     void (*k)(const Params) = p.classes <= 32 * V ? warp_kernel<XT, 1> : p.classes <= 64 * V ? warp_kernel<XT, 2> : warp_kernel<XT, 4>;
