@@ -527,3 +527,18 @@ def test_a_layer_in_host_memory_is_not_run():
             layer.run(x, torch.empty((4, 40), dtype=torch.float16), stream=stream)
         with pytest.raises(ValueError, match="CUDA"):
             layer.run(x, stream=stream)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,scale,group,zeros", [(torch.float16, torch.float32, 32, True), (torch.bfloat16, torch.float32, 32, True), (torch.float16, torch.float16, 128, False),
+                                                     (torch.bfloat16, torch.bfloat16, 64, True), (torch.bfloat16, torch.float32, 128, False)])
+@pytest.mark.parametrize("rows,cin", [(256, 304), (256, 515), (600, 72), (129, 640)])
+def test_tiles_of_256_rows(dtype, scale, group, zeros, rows, cin):
+    """Outputs enough for every SM: the largest tiles, whose stages are the fewest."""
+    cout = 9700
+    layer, w = make(cin, cin, cout, group, dtype, scale, zeros)
+    x = rows_of(rows, rows, cin, dtype)
+    got = layer.run(x.cuda()).double().cpu()
+    want, bound = two_part_bound(x, w, group)
+    assert ((got - want).abs() <= bound).all(), ((got - want).abs() / bound).max()
+    assert api.gi_device_status() == 0
